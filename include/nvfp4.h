@@ -439,6 +439,86 @@ nvfp4_status nvfp4_osci_sparse_suppress(float* W, int64_t ldw, int64_t C, int64_
                                         const int32_t* idx, const float* D_M, const float* D_Q, float tau,
                                         unsigned long long* n_reset, void* workspace, size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * nvfp4_gemv -- a few tokens times the weights of the layer, the product of token-by-token answering. (The paper trains; this is the
+ * forward product of Sec. 2.3 with X as it is instead of Q1(X), and the outlier channels of Sec. 4.2 beside it.)
+ *
+ *   Y[m, n] = sum_k X[m, kept(k)] W-hat[n, k]  (+ sum_j X[m, outlier_cols[j]] W_out[n, j])  (+ bias[n]),  W-hat = P * S_block * S_global
+ *
+ *   X_bf16   [M, D], leading dimension ldx. Any M; every 32 tokens are one pass over the weights, meant for few tokens.
+ *   W        operand [N, K] along the input channels in either scale layout and any gs_mode (nvfp4_quantize of the weights along AXIS_ROW,
+ *            nvfp4_quantize_w16x16, or nvfp4_saved.qw of a forward call).
+ *   n_out    0: K == D, and the three arguments after W are not looked at. Otherwise K + n_out == D; keep_cols [K] and outlier_cols [n_out]
+ *            (device int32) say which column of X an operand column or an outlier stands for, W_out is BF16 [N, nvfp4_outlier_pad(n_out)],
+ *            16-byte aligned, as in nvfp4_saved (its columns from n_out on are multiplied by zero: finite). A column outside
+ *            0 .. D-1 is read as NaN.
+ *   bias     optional BF16 [N].
+ *   Y        [M, N], leading dimension ldy, dtype y_dtype, 16-byte aligned rows. Columns from N on are left as they were.
+ * Products of X and P * S_block are exact, sums are FP32 in an order that M does not change; an element of X below 2^-28 of its token's
+ * largest in 128 columns may lose up to 2^-39 of that largest one. Non-finite elements of X give non-finite results of their token.
+ * Errors: NULL / ENUM / SHAPE (K + n_out != D, K <= 0) / LIMIT (M > 2097120, D > 2^30) / ALIGN / ARCH; nothing is launched on an error.
+ * --------------------------------------------------------------------------------------------------------- */
+nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, const nvfp4_operand* W, const int32_t* keep_cols,
+                        const int32_t* outlier_cols, int64_t n_out, const void* W_out, const void* bias_bf16, void* Y, int32_t y_dtype,
+                        int64_t ldy, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------
+ * Activation checkpoints in 8 bits: what the steps around the linears keep for backward, in half of BF16's bytes. (The linears themselves
+ * keep their FP4 operands, nvfp4_saved. The paper has no counterpart; the format is this library's.)
+ *
+ * A matrix [R, K] in groups of 32 elements along K (the last of a row may be shorter). With a = max |x| over the finite elements of a group
+ * and e the smallest integer >= -117 with a <= 448 * 2^e:
+ *     code = E4M3(x * 2^-e)  (round to nearest, ties to even),   scale byte = e + 127,   value = code * 2^e  (exact in FP32 and BF16).
+ * A non-finite element becomes NaN; values above 1.9375 * 2^127 round to infinity.
+ *   codes  : uint8 [R, ld], ld = nvfp4_ckpt8_ld(K) = K rounded up to 32; codes past K are 0. 16-byte aligned.
+ *   scales : uint8 [R, ld / 32].
+ * The struct lives on the host, both arrays on the device; R and K are inputs and validated.
+ *   nvfp4_ckpt8_pack    X [R, K] of x_dtype, leading dimension ldx, 16-byte aligned rows -> *out.
+ *   nvfp4_ckpt8_unpack  *in -> X of x_dtype; columns of X from K on are left as they were.
+ * Errors: NULL / ENUM / SHAPE / ALIGN / LIMIT (K > 2^24, or more than 2^42 elements) / ARCH; nothing is launched on an error.
+ * --------------------------------------------------------------------------------------------------------- */
+typedef struct {
+  uint8_t* codes;
+  uint8_t* scales;
+  int64_t R, K;
+} nvfp4_ckpt8;
+int64_t nvfp4_ckpt8_ld(int64_t K);
+nvfp4_status nvfp4_ckpt8_pack(const void* X, int32_t x_dtype, int64_t ldx, int64_t R, int64_t K, const nvfp4_ckpt8* out, void* stream);
+nvfp4_status nvfp4_ckpt8_unpack(const nvfp4_ckpt8* in, void* X, int32_t x_dtype, int64_t ldx, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------
+ * SwiGLU, the input of the down projection: h = g s u with s = 1 / (1 + exp(-g)); dg = dh u s (1 + g (1 - s)), du = dh g s.
+ * All matrices BF16 [T, D] with their own leading dimensions and 16-byte aligned rows; FP32 arithmetic, one rounding per result.
+ *   fwd: g8 and u8 both NULL, or both checkpoints [T, D] to be filled with G and U beside H. H may be G or U.
+ *   bwd: with g8 and u8 the values are the checkpoints' (G and U are not looked at), else G's and U's. dG and dU may be dH, G or U, but not
+ *        one another.
+ * Errors as for the checkpoints (SHAPE also where only one of g8, u8 is given).
+ * --------------------------------------------------------------------------------------------------------- */
+nvfp4_status nvfp4_swiglu_fwd(const void* G, int64_t ldg, const void* U, int64_t ldu, int64_t T, int64_t D, void* H, int64_t ldh,
+                              const nvfp4_ckpt8* g8, const nvfp4_ckpt8* u8, void* stream);
+nvfp4_status nvfp4_swiglu_bwd(const void* dH, int64_t lddh, const void* G, int64_t ldg, const void* U, int64_t ldu, const nvfp4_ckpt8* g8,
+                              const nvfp4_ckpt8* u8, int64_t T, int64_t D, void* dG, int64_t lddg, void* dU, int64_t lddu, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------
+ * Layer norm over the rows of X [T, D], D <= 16384 (NVFP4_ERR_LIMIT beyond): the step in front of a block's linears.
+ *     m = mean(x), v = mean((x - m)^2), r = 1 / sqrt(v + eps), y = (x - m) r gamma + beta
+ *     xh = (x - m) r, h = dy gamma:   dx = r (h - mean(h) - xh mean(h xh)),   dgamma = sum_t dy xh,   dbeta = sum_t dy
+ *   X      x_dtype (BF16 or FP32); gamma, beta (optional) param_dtype [D], 16-byte aligned; Y and dY BF16; dX of x_dtype.
+ *   stats  FP32 [T, 2], 8-byte aligned: (m, r) of every row, what backward reads. Optional in forward.
+ *   x8     optional. Forward: the checkpoint of X is written too. Backward: x is the checkpoint's (X is not looked at; m and r remain
+ *          those of X).
+ *   dgamma, dbeta (NULL: not wanted)  dparam_dtype [D], written also for T = 0. Sums are FP32 in a fixed order.
+ *   workspace (backward): nvfp4_layernorm_bwd_workspace_bytes(T, D) bytes, 16-byte aligned.
+ * dX may be dY or X where their types are the same. Rows and columns beyond [T, D] are left as they were.
+ * Errors: NULL / ENUM / SHAPE (T < 0, D <= 0, eps < 0 or NaN, a checkpoint of another shape) / LIMIT / ALIGN / WORKSPACE / ARCH.
+ * --------------------------------------------------------------------------------------------------------- */
+nvfp4_status nvfp4_layernorm_fwd(const void* X, int32_t x_dtype, int64_t ldx, int64_t T, int64_t D, const void* gamma, const void* beta,
+                                 int32_t param_dtype, float eps, void* Y, int64_t ldy, float* stats, const nvfp4_ckpt8* x8, void* stream);
+size_t nvfp4_layernorm_bwd_workspace_bytes(int64_t T, int64_t D);
+nvfp4_status nvfp4_layernorm_bwd(const void* dY, int64_t lddy, const void* X, int32_t x_dtype, int64_t ldx, const nvfp4_ckpt8* x8, int64_t T,
+                                 int64_t D, const void* gamma, int32_t param_dtype, const float* stats, void* dX, int64_t lddx, void* dgamma,
+                                 void* dbeta, int32_t dparam_dtype, void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,14 +9,14 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnvfp4_b200.so")
-SOURCES = ["api.cu", "quantize.cu", "gemm.cu", "hp.cu", "noalloc.cu", "calib.cu", "osci.cu", "w16.cu", "fp6.cu"]
+SOURCES = ["api.cu", "quantize.cu", "gemm.cu", "hp.cu", "noalloc.cu", "calib.cu", "osci.cu", "w16.cu", "fp6.cu", "act.cu", "norm.cu", "gemv.cu"]
 # measurement aids (the tensor-core issue loop): a library of their own, loaded by the benchmark only
 MEASURE_LIB = os.path.join(HERE, "libnvfp4_measure.so")
 MEASURE_SOURCES = ["probe.cu"]
 # the autograd node of NVFP4Linear: a Python module that calls the library (found beside it) between torch's allocator and engine
 NODE_LIB = os.path.join(HERE, "_node.so")
 NODE_SOURCES = ["torch_node.cpp"]
-HEADERS = ["nvfp4_device.cuh", "nvfp4_internal.h", "nvfp4_tc.cuh", os.path.join("..", "..", "include", "nvfp4.h"),
+HEADERS = ["nvfp4_device.cuh", "act8.cuh", "nvfp4_internal.h", "nvfp4_tc.cuh", os.path.join("..", "..", "include", "nvfp4.h"),
            os.path.join("..", "..", "include", "nvfp4_measure.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

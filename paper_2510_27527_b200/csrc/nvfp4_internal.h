@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <utility>
 
 namespace nvfp4 {
 
@@ -105,10 +106,11 @@ inline cudaError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block
 
 // The same with thread-block clusters of `cluster_x` CTAs along x (a divisor of grid.x).
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_kernel_cluster(void (*kernel)(KArgs...), dim3 grid, unsigned cluster_x, dim3 block, cudaStream_t st, Args&&... args) {
+inline cudaError_t launch_kernel_cluster_smem(void (*kernel)(KArgs...), dim3 grid, unsigned cluster_x, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -120,6 +122,10 @@ inline cudaError_t launch_kernel_cluster(void (*kernel)(KArgs...), dim3 grid, un
   cfg.numAttrs = 2;
   g_launch_count.fetch_add(1, std::memory_order_relaxed);
   return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_kernel_cluster(void (*kernel)(KArgs...), dim3 grid, unsigned cluster_x, dim3 block, cudaStream_t st, Args&&... args) {
+  return launch_kernel_cluster_smem(kernel, grid, cluster_x, block, 0, st, std::forward<Args>(args)...);
 }
 // Shape of an amax launch that writes at most n_words words (cells_write): CTAs along x and CTAs per cluster.
 struct AmaxGrid {
