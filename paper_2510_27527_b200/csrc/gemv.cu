@@ -10,8 +10,10 @@
 // than 2^-39 of it. Every 128 k the FP32 result of the instructions is added to FP32 sums with the product of that power of two and the
 // weights' global scale, which is constant there in every scale mode.
 // The outlier channels go through BF16 instructions, 32 of them per step, with the same rows.
-// A CTA takes 64 rows: 16 of each 32 of a 128-row tile, because that is whose scale bytes lie together. The k axis is split over the warps of a CTA
-// and over the CTAs of a cluster, whose sums are added through distributed shared memory in a fixed order, one that M does not change.
+// A CTA is four warps of 32 rows, a 128-row tile, because that is whose scale bytes lie together. A warp brings its rows' codes and scales
+// through a ring of its own in shared memory (asynchronous copies, kStages pieces ahead, no barrier between warps).
+// The k axis is split over the CTAs of a cluster, whose sums are added through distributed shared memory in a fixed order, one that M does
+// not change.
 #include "../../include/nvfp4.h"
 
 #include "act8.cuh"
@@ -21,10 +23,12 @@ namespace nvfp4 {
 
 namespace {
 
-constexpr int kRows = 64;        // weight rows of a CTA
-constexpr int kKWarps = 2;       // warps along k
-constexpr int kThreads = 4 * kKWarps * 32;
-constexpr int kPrefetch = 4;     // items in flight per warp
+constexpr int kRows = 128;       // weight rows of a CTA, 32 of a warp
+constexpr int kThreads = 128;
+constexpr int kStages = 4;       // pieces in flight per warp
+constexpr int kStageBytes = 2048 + 256 + 128;  // 32 rows of 64 bytes, their scales, their global scales
+constexpr int kSfAt = 2048, kGsAt = kSfAt + 256;
+constexpr int kRingBytes = 4 * kStages * kStageBytes;
 constexpr int kMaxTokens = 32;   // of one pass over the weights
 constexpr int kMaxCluster = 8;
 constexpr int kXBytes = 64 * 1024;  // of staged X, at most
@@ -48,15 +52,21 @@ struct GemvArgs {
   int seg;               // items staged at a time
 };
 
-struct Item {  // what a lane holds of one item
-  uint4 w0, w1;
-  uint32_t s0, s1;  // two scale bytes each
-  float g0, g1;
-};
-
-__device__ __forceinline__ uint4 load_stream(const void* p) {
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copy4(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ uint4 shared16(uint32_t at) {
   uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t shared_u16(uint32_t at) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float shared_f32(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
   return v;
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -117,177 +127,228 @@ __device__ __forceinline__ uint4 x8(const uint16_t* row, const int32_t* cols, in
   return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
 }
 
-template <int MT>  // instructions' widths of eight tokens
+template <int MT, bool B128, bool TILED>  // MT: instructions' widths of eight tokens
 __global__ void __launch_bounds__(kThreads) gemv_kernel(GemvArgs a) {
   pdl_prologue();
   extern __shared__ __align__(16) uint8_t smem[];
   constexpr int TOK = 8 * MT;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int rowset = wid & 3, kw = wid >> 2;
-  const int S = (int)cluster_ctas(), rank = (int)(blockIdx.x % (uint32_t)S);
-  const int64_t rb = blockIdx.x / (uint32_t)S;
+  uint32_t S, rank, rb;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(S));
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm("mov.u32 %0, %%clusterid.x;" : "=r"(rb));
   const int64_t m0 = (int64_t)blockIdx.y * kMaxTokens;
   const int Mg = (int)min((int64_t)kMaxTokens, a.M - m0);
-  const int64_t row0 = (rb >> 1) * 128 + rowset * 32 + (rb & 1) * 16 + g;
-  const int64_t r0 = min(row0, a.N - 1), r1 = min(row0 + 8, a.N - 1);  // (rows past the end repeat the last one and are not stored)
+  const int64_t row_w = (int64_t)rb * kRows + wid * 32;  // the warp's first row
+  const int64_t last = a.N - 1;                          // (rows past the end repeat the last one and are not stored)
+  const int64_t rs = min(row_w + lane, last);            // whose scales this lane brings
   const int Kp = (a.K + 127) & ~127;
   const int64_t nb = Kp >> 4, nbp = (nb + 15) & ~(int64_t)15;
 
-  uint8_t* xs = smem;                                                       // [item][4][token][4] 16 bytes
-  float* xscale = reinterpret_cast<float*>(smem + (size_t)a.seg * 256 * Mg);  // [item][TOK]
-  float* red = xscale + a.seg * TOK;                                        // [kw][TOK][kRows]
+  uint8_t* xs = smem + kRingBytes;                                             // [piece][4][token][4] 16 bytes, then one piece of zeros
+  float* xscale = reinterpret_cast<float*>(xs + (size_t)(a.seg + 1) * 256 * Mg);  // [piece][TOK]
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + wid * (kStages * kStageBytes);
+  const uint32_t xs_at = (uint32_t)__cvta_generic_to_shared(xs), xscale_at = (uint32_t)__cvta_generic_to_shared(xscale);
 
-  const int i_begin = (int)((int64_t)rank * a.n_items / S), i_end = (int)((int64_t)(rank + 1) * a.n_items / S);
-  const uint8_t *c0 = a.codes + r0 * (Kp >> 1) + t * 16, *c1 = a.codes + r1 * (Kp >> 1) + t * 16;
-  const uint16_t *o0 = a.W_out + r0 * a.Kh + t * 8, *o1 = a.W_out + r1 * a.Kh + t * 8;
-  const uint8_t* sf0 = a.tiled ? a.sf + sf_tiled_offset(r0, 2 * t, nbp) : a.sf + r0 * nb + 2 * t;
-  const uint8_t* sf1 = a.tiled ? a.sf + sf_tiled_offset(r1, 2 * t, nbp) : a.sf + r1 * nb + 2 * t;
-  const int sf_step = a.tiled ? 1024 : 8;  // bytes from one item to the next
-  const bool b128 = a.gs_mode == kGsBlock128;
-  const float* gs0 = a.gscale + (b128 ? r0 * (Kp >> 7) : a.gs_mode == kGsRow ? r0 : 0);
-  const float* gs1 = a.gscale + (b128 ? r1 * (Kp >> 7) : a.gs_mode == kGsRow ? r1 : 0);
+  const int i_begin = (int)(rank * (uint32_t)a.n_items / S), i_end = (int)((rank + 1) * (uint32_t)a.n_items / S);
+  const uint8_t *c[4], *o[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t r = min(row_w + g + 8 * j, last);
+    c[j] = a.codes + r * (Kp >> 1) + t * 16;
+    o[j] = reinterpret_cast<const uint8_t*>(a.W_out) + r * a.Kh * 2 + t * 16;
+  }
+  const uint8_t* sf = a.sf + (TILED ? (int64_t)sf_tiled_offset(rs, 0, nbp) : rs * nb);
+  const float* gs = a.gscale + (B128 ? rs * (Kp >> 7) : 0);
+  float gv[4] = {};
+  if (!B128)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) gv[j] = a.gscale[a.gs_mode == kGsRow ? min(row_w + g + 8 * j, last) : 0];
 
-  auto load = [&](Item& q, int i) {
-    if (i < a.n_codes) {
-      q.w0 = load_stream(c0 + (int64_t)i * 64);
-      q.w1 = load_stream(c1 + (int64_t)i * 64);
-      q.s0 = *reinterpret_cast<const uint16_t*>(sf0 + (int64_t)i * sf_step);
-      q.s1 = *reinterpret_cast<const uint16_t*>(sf1 + (int64_t)i * sf_step);
-      q.g0 = gs0[b128 ? i : 0];
-      q.g1 = gs1[b128 ? i : 0];
-    } else {
-      q.w0 = load_stream(o0 + (int64_t)(i - a.n_codes) * 32);
-      q.w1 = load_stream(o1 + (int64_t)(i - a.n_codes) * 32);
+  // piece i into its place in the ring; one group of copies, empty past the end
+  auto fetch = [&](int i) {
+    if (i < i_end) {
+      const uint32_t to = ring + (uint32_t)(i & (kStages - 1)) * kStageBytes;
+      if (i < a.n_codes) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) copy16(to + j * 512 + lane * 16, c[j] + (int64_t)i * 64);
+        copy4(to + kSfAt + lane * 8, sf + (int64_t)i * (TILED ? 1024 : 8));  // four blocks' scales, and the next four's
+        copy4(to + kSfAt + lane * 8 + 4, sf + (int64_t)i * (TILED ? 1024 : 8) + (TILED ? 512 : 4));
+        if (B128) copy4(to + kGsAt + lane * 4, gs + i);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) copy16(to + j * 512 + lane * 16, o[j] + (int64_t)(i - a.n_codes) * 64);
+      }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
+#pragma unroll
+  for (int p = 0; p < kStages; ++p) fetch(i_begin + p);
+  for (int i = threadIdx.x; i < 16 * Mg; i += kThreads) *reinterpret_cast<uint4*>(xs + (size_t)a.seg * 256 * Mg + i * 16) = make_uint4(0, 0, 0, 0);
 
-  float acc[MT][4] = {};
-  Item q[kPrefetch];
-  for (int s0 = i_begin; s0 < i_end; s0 += a.seg) {
-    const int n_seg = min(a.seg, i_end - s0);
+  // where this lane's X lies in a piece, for each eight tokens; tokens that do not exist are read from the zeros
+  uint32_t b_at[MT], b_step[MT];
 #pragma unroll
-    for (int p = 0; p < kPrefetch; ++p)
-      if (kw + p * kKWarps < n_seg) load(q[p], s0 + kw + p * kKWarps);
-    // X: 16 lanes take a token's 128 values of a piece (or the 32 of a step: 4 lanes of them), eight each
-    {
-      const int l16 = lane & 15;
-      for (int u0 = wid * 2; u0 < n_seg * Mg; u0 += kThreads / 16) {  // (a warp's two halves stay together)
-        const int u = u0 + (lane >> 4);
-        const bool live = u < n_seg * Mg;
-        const int it = live ? u / Mg : 0, m = live ? u - it * Mg : 0, i = s0 + it;
-        const uint16_t* row = a.X + (m0 + m) * a.ldx;
-        const bool code = i < a.n_codes;
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (live && code) w = x8(row, a.keep, i * 128 + l16 * 8, a.K, a.D);
-        if (live && !code && l16 < 4) w = x8(row, a.outl, (i - a.n_codes) * 32 + l16 * 8, a.n_out, a.D);
-        uint32_t m2 = amax16x2(amax16x2(w.x, w.y), amax16x2(w.z, w.w));
-        float v[8], big = fmaxf(fabsf(bf16_lo(m2)), fabsf(bf16_hi(m2)));
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) big = fmaxf(big, __shfl_xor_sync(0xFFFFFFFFu, big, o));
-        const uint32_t e = max(__float_as_uint(big) >> 23, 15u);
-        if (code) {
-          const float to = __uint_as_float((268u - e) << 23);  // 2^(141 - e)
-          bf16x8_values(w, v);
-          uint32_t h[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const __half2 p = __floats2half2_rn(v[2 * j] * to, v[2 * j + 1] * to);
-            h[j] = *reinterpret_cast<const uint32_t*>(&p);
-          }
-          w = make_uint4(h[0], h[1], h[2], h[3]);
-        }
-        if (live) {
-          uint8_t* at = xs + (size_t)it * 256 * Mg;
-          if (code) {
-            *reinterpret_cast<uint4*>(at + (((l16 & 3) * Mg + m) * 4 + (l16 >> 2)) * 16) = w;
-            if (l16 == 0) xscale[it * TOK + m] = __uint_as_float((e - 14u) << 23);  // 2^(e - 141)
-          } else if (l16 < 4) {
-            *reinterpret_cast<uint4*>(at + (m * 4 + l16) * 16) = w;
-          }
-        }
-      }
-    }
-    __syncthreads();
-    for (int j = kw; j < n_seg; j += kPrefetch * kKWarps) {
-#pragma unroll
-      for (int p = 0; p < kPrefetch; ++p) {
-        const int it = j + p * kKWarps;
-        if (it < n_seg) {
-          const uint8_t* at = xs + (size_t)it * 256 * Mg;
-          float d[MT][4] = {};
-          if (s0 + it < a.n_codes) {
-            uint32_t sa[2], sb[2];
-            scales2(q[p].s0, sa);
-            scales2(q[p].s1, sb);
-            const uint32_t wa[4] = {q[p].w0.x, q[p].w0.y, q[p].w0.z, q[p].w0.w}, wb[4] = {q[p].w1.x, q[p].w1.y, q[p].w1.z, q[p].w1.w};
-#pragma unroll
-            for (int wd = 0; wd < 4; ++wd) {
-              uint32_t ha[4], hb[4];
-              weights8(wa[wd], sa[wd >> 1], ha);
-              weights8(wb[wd], sb[wd >> 1], hb);
-#pragma unroll
-              for (int n = 0; n < MT; ++n) {
-                uint4 b = make_uint4(0, 0, 0, 0);
-                if (n * 8 + g < Mg) b = *reinterpret_cast<const uint4*>(at + ((wd * Mg + n * 8 + g) * 4 + t) * 16);
-                mma_f16(d[n], ha[0], hb[0], ha[1], hb[1], b.x, b.y);
-                mma_f16(d[n], ha[2], hb[2], ha[3], hb[3], b.z, b.w);
-              }
-            }
-#pragma unroll
-            for (int n = 0; n < MT; ++n) {
-              const float2 xsc = *reinterpret_cast<const float2*>(xscale + it * TOK + n * 8 + 2 * t);
-              acc[n][0] = fmaf(d[n][0], xsc.x * q[p].g0, acc[n][0]);
-              acc[n][1] = fmaf(d[n][1], xsc.y * q[p].g0, acc[n][1]);
-              acc[n][2] = fmaf(d[n][2], xsc.x * q[p].g1, acc[n][2]);
-              acc[n][3] = fmaf(d[n][3], xsc.y * q[p].g1, acc[n][3]);
-            }
-          } else {
-#pragma unroll
-            for (int n = 0; n < MT; ++n) {
-              uint4 b = make_uint4(0, 0, 0, 0);
-              if (n * 8 + g < Mg) b = *reinterpret_cast<const uint4*>(at + ((n * 8 + g) * 4 + t) * 16);
-              mma_bf16(d[n], q[p].w0.x, q[p].w1.x, q[p].w0.y, q[p].w1.y, b.x, b.y);
-              mma_bf16(d[n], q[p].w0.z, q[p].w1.z, q[p].w0.w, q[p].w1.w, b.z, b.w);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[n][e] += d[n][e];
-            }
-          }
-          if (it + kPrefetch * kKWarps < n_seg) load(q[p], s0 + it + kPrefetch * kKWarps);
-        }
-      }
-    }
-    __syncthreads();
+  for (int n = 0; n < MT; ++n) {
+    const bool live = n * 8 + g < Mg;
+    b_at[n] = xs_at + (live ? ((n * 8 + g) * 4 + t) * 16 : a.seg * 256 * Mg);
+    b_step[n] = live ? 256 * Mg : 0;
   }
 
-  // the warps' sums, then the cluster's
+  float acc[2][MT][4] = {};
+  for (int s0 = i_begin; s0 < i_end; s0 += a.seg) {
+    const int n_seg = min(a.seg, i_end - s0);
+    if (s0 > i_begin) __syncthreads();
+    // X: 16 lanes take a token's 128 values of a piece (or the 32 of an outlier step: 4 lanes of them), eight each; kAhead loads at a time
+    {
+      constexpr int kAhead = 4;
+      const int l16 = lane & 15, n_units = n_seg * Mg;
+      for (int u0 = wid * 2 + (lane >> 4); u0 - (lane >> 4) < n_units; u0 += kAhead * (kThreads / 16)) {  // (a warp's two halves stay together)
+        uint4 w[kAhead];
+        int it[kAhead], m[kAhead];
+#pragma unroll
+        for (int p = 0; p < kAhead; ++p) {
+          const int u = u0 + p * (kThreads / 16);
+          w[p] = make_uint4(0, 0, 0, 0);
+          it[p] = m[p] = 0;
+          if (u < n_units) {
+            it[p] = Mg == 1 ? u : u / Mg;
+            m[p] = u - it[p] * Mg;
+            const int i = s0 + it[p];
+            const uint16_t* row = a.X + (m0 + m[p]) * a.ldx;
+            if (i < a.n_codes)
+              w[p] = x8(row, a.keep, i * 128 + l16 * 8, a.K, a.D);
+            else if (l16 < 4)
+              w[p] = x8(row, a.outl, (i - a.n_codes) * 32 + l16 * 8, a.n_out, a.D);
+          }
+        }
+#pragma unroll
+        for (int p = 0; p < kAhead; ++p) {
+          const int u = u0 + p * (kThreads / 16);
+          const uint32_t m2 = amax16x2(amax16x2(w[p].x, w[p].y), amax16x2(w[p].z, w[p].w));
+          uint32_t big = max(m2 & 0x7FFFu, (m2 >> 16) & 0x7FFFu);  // (bit patterns of magnitudes are ordered like them)
+#pragma unroll
+          for (int o = 1; o < 16; o <<= 1) big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, o));
+          if (u >= n_units) continue;
+          const uint32_t e = max(big >> 7, 15u);
+          uint8_t* at = xs + (size_t)it[p] * 256 * Mg;
+          if (s0 + it[p] < a.n_codes) {
+            const float to = __uint_as_float((268u - e) << 23);  // 2^(141 - e)
+            float v[8];
+            bf16x8_values(w[p], v);
+            uint32_t h[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const __half2 q = __floats2half2_rn(v[2 * j] * to, v[2 * j + 1] * to);
+              h[j] = *reinterpret_cast<const uint32_t*>(&q);
+            }
+            *reinterpret_cast<uint4*>(at + (((l16 & 3) * Mg + m[p]) * 4 + (l16 >> 2)) * 16) = make_uint4(h[0], h[1], h[2], h[3]);
+            if (l16 == 0) xscale[it[p] * TOK + m[p]] = __uint_as_float((e - 14u) << 23);  // 2^(e - 141)
+          } else if (l16 < 4) {
+            *reinterpret_cast<uint4*>(at + (m[p] * 4 + l16) * 16) = w[p];
+          }
+        }
+      }
+    }
+    __syncthreads();
+    uint32_t b_now[MT];
+#pragma unroll
+    for (int n = 0; n < MT; ++n) b_now[n] = b_at[n];
+    uint32_t xsc_now = xscale_at + 8 * t;
+    const int s_codes = min(s0 + n_seg, a.n_codes);
+    int i = s0;
+#pragma unroll 1
+    for (; i < s_codes; ++i) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+      __syncwarp();
+      const uint32_t at = ring + (uint32_t)(i & (kStages - 1)) * kStageBytes;
+      uint32_t wv[4][4], sc[4][2];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint4 w = shared16(at + j * 512 + lane * 16);
+        wv[j][0] = w.x; wv[j][1] = w.y; wv[j][2] = w.z; wv[j][3] = w.w;
+        scales2(shared_u16(at + kSfAt + (g + 8 * j) * 8 + t * 2), sc[j]);
+        if (B128) gv[j] = shared_f32(at + kGsAt + (g + 8 * j) * 4);
+      }
+      __syncwarp();
+      fetch(i + kStages);
+      float d[2][MT][4] = {};
+#pragma unroll
+      for (int wd = 0; wd < 4; ++wd) {
+        uint32_t h[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) weights8(wv[j][wd], sc[j][wd >> 1], h[j]);
+#pragma unroll
+        for (int n = 0; n < MT; ++n) {
+          const uint4 b = shared16(b_now[n] + (uint32_t)(wd * Mg) * 64);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            mma_f16(d[k][n], h[2 * k][0], h[2 * k + 1][0], h[2 * k][1], h[2 * k + 1][1], b.x, b.y);
+            mma_f16(d[k][n], h[2 * k][2], h[2 * k + 1][2], h[2 * k][3], h[2 * k + 1][3], b.z, b.w);
+          }
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < MT; ++n) {
+        const float x0 = shared_f32(xsc_now + n * 32), x1 = shared_f32(xsc_now + n * 32 + 4);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          acc[k][n][0] = fmaf(d[k][n][0], x0 * gv[2 * k], acc[k][n][0]);
+          acc[k][n][1] = fmaf(d[k][n][1], x1 * gv[2 * k], acc[k][n][1]);
+          acc[k][n][2] = fmaf(d[k][n][2], x0 * gv[2 * k + 1], acc[k][n][2]);
+          acc[k][n][3] = fmaf(d[k][n][3], x1 * gv[2 * k + 1], acc[k][n][3]);
+        }
+        b_now[n] += b_step[n];
+      }
+      xsc_now += TOK * 4;
+    }
+#pragma unroll 1
+    for (; i < s0 + n_seg; ++i) {  // outlier channels
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+      __syncwarp();
+      const uint32_t at = ring + (uint32_t)(i & (kStages - 1)) * kStageBytes;
+      uint4 w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = shared16(at + j * 512 + lane * 16);
+      __syncwarp();
+      fetch(i + kStages);
+#pragma unroll
+      for (int n = 0; n < MT; ++n) {
+        const uint4 b = shared16(b_now[n]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float d[4] = {};
+          mma_bf16(d, w[2 * k].x, w[2 * k + 1].x, w[2 * k].y, w[2 * k + 1].y, b.x, b.y);
+          mma_bf16(d, w[2 * k].z, w[2 * k + 1].z, w[2 * k].w, w[2 * k + 1].w, b.z, b.w);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[k][n][e] += d[e];
+        }
+        b_now[n] += b_step[n];
+      }
+    }
+  }
+
+  // the cluster's sums, where the rings were
+  __syncthreads();
+  float* red = reinterpret_cast<float*>(smem);  // [TOK][kRows]
 #pragma unroll
   for (int n = 0; n < MT; ++n)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) red[(kw * TOK + n * 8 + 2 * t + (e & 1)) * kRows + rowset * 16 + g + (e >> 1) * 8] = acc[n][e];
+    for (int e = 0; e < 8; ++e) red[(n * 8 + 2 * t + (e & 1)) * kRows + wid * 32 + g + (e >> 1) * 8] = acc[e >> 2][n][e & 3];
   __syncthreads();
-  if (kKWarps > 1) {
-    for (int i = threadIdx.x; i < Mg * kRows; i += kThreads) {
-      float s = red[i];
-#pragma unroll
-      for (int k = 1; k < kKWarps; ++k) s += red[k * TOK * kRows + i];
-      red[i] = s;
-    }
-    __syncthreads();
-  }
   if (S > 1) {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   }
-  const int rows = kRows / S;  // that this CTA finishes
-  for (int i = threadIdx.x; i < Mg * rows; i += kThreads) {
-    const int m = i / rows, r = rank * rows + (i - m * rows);
+  for (int i = rank * kThreads + threadIdx.x; i < Mg * kRows; i += S * kThreads) {
+    const int m = i / kRows, r = i % kRows;
     const float* p = red + m * kRows + r;
     float s = 0.0f;
     if (S == 1)
       s = *p;
     else
-      for (int k = 0; k < S; ++k) s += load_cluster(p, (uint32_t)k);
-    const int64_t n = (rb >> 1) * 128 + (r >> 4) * 32 + (rb & 1) * 16 + (r & 15);
+      for (uint32_t k = 0; k < S; ++k) s += load_cluster(p, k);
+    const int64_t n = (int64_t)rb * kRows + r;
     if (n < a.N) {
       if (a.bias) s += bf16_bits_to_float(a.bias[n]);
       if (a.y_f32)
@@ -302,15 +363,21 @@ __global__ void __launch_bounds__(kThreads) gemv_kernel(GemvArgs a) {
   }
 }
 
-template <int MT>
+template <int MT, bool B128, bool TILED>
 cudaError_t launch_gemv(GemvArgs a, int64_t row_ctas, int S, cudaStream_t st) {
   const int Mg = (int)std::min<int64_t>(a.M, kMaxTokens);
   const int per_cta = (a.n_items + S - 1) / S;
   a.seg = std::max(1, std::min(per_cta, kXBytes / (256 * Mg)));
-  const size_t smem = (size_t)a.seg * (256 * Mg + 8 * MT * 4) + (size_t)kKWarps * 8 * MT * kRows * 4;
-  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(gemv_kernel<MT>), smem);
+  const size_t smem = kRingBytes + (size_t)(a.seg + 1) * 256 * Mg + (size_t)a.seg * 8 * MT * 4;
+  auto kernel = gemv_kernel<MT, B128, TILED>;
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
   if (e != cudaSuccess) return e;
-  return launch_kernel_cluster_smem(gemv_kernel<MT>, dim3((unsigned)(row_ctas * S), (unsigned)((a.M + kMaxTokens - 1) / kMaxTokens)), (unsigned)S, dim3(kThreads), smem, st, a);
+  return launch_kernel_cluster_smem(kernel, dim3((unsigned)(row_ctas * S), (unsigned)((a.M + kMaxTokens - 1) / kMaxTokens)), (unsigned)S, dim3(kThreads), smem, st, a);
+}
+template <int MT>
+cudaError_t launch_gemv(const GemvArgs& a, int64_t row_ctas, int S, cudaStream_t st) {
+  if (a.gs_mode == kGsBlock128) return a.tiled ? launch_gemv<MT, true, true>(a, row_ctas, S, st) : launch_gemv<MT, true, false>(a, row_ctas, S, st);
+  return a.tiled ? launch_gemv<MT, false, true>(a, row_ctas, S, st) : launch_gemv<MT, false, false>(a, row_ctas, S, st);
 }
 
 }  // namespace
@@ -356,10 +423,10 @@ nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, c
   a.ldy = ldy;
   a.n_codes = (int)(nvfp4_padded_k(W->K) / 128);
   a.n_items = a.n_codes + (n_out > 0 ? a.Kh / 32 : 0);
-  // CTAs along k: as many as give every SM up to four of them, while every warp keeps an item
-  const int64_t row_ctas = (W->R + 127) / 128 * 2, most = (int64_t)device_sm_count() * 4;
+  // CTAs along k
+  const int64_t row_ctas = (W->R + kRows - 1) / kRows, sms = device_sm_count();
   int S = 1;
-  while (S < kMaxCluster && row_ctas * S * 2 <= most && a.n_items >= 2 * S * kKWarps) S *= 2;
+  while (S < kMaxCluster && row_ctas * S * 2 <= sms * 4 && a.n_items >= 2 * S) S *= 2;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = M <= 8 ? launch_gemv<1>(a, row_ctas, S, st) : M <= 16 ? launch_gemv<2>(a, row_ctas, S, st) : launch_gemv<4>(a, row_ctas, S, st);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
