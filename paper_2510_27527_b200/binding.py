@@ -15,6 +15,8 @@ from dataclasses import dataclass
 import numpy as np
 import torch
 
+from .build import node_tag
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libnvfp4_b200.so")
 if not os.path.exists(LIB_PATH):
@@ -158,6 +160,14 @@ def measure_lib():
             getattr(_measure_lib, name).restype = res
             getattr(_measure_lib, name).argtypes = args
     return _measure_lib
+
+
+try:  # (linked with the library above)
+    from . import _node
+    if getattr(_node, "built_for", None) != node_tag():  # (it may load all the same)
+        raise ImportError(f"{_node.__file__} is not for {node_tag()}")
+except ImportError as e:
+    raise ImportError(f"{e}: build it with `python -m paper_2510_27527_b200.build`") from e
 
 
 class Nvfp4Error(RuntimeError):
@@ -837,84 +847,20 @@ def fp6_linear_bwd(dY: torch.Tensor, saved, seed: int = 0, dx_dtype: int = DT_BF
 # ------------------------------------------------------------------------------------------------------------
 # around the linears of a block: few-token products, 8-bit activation checkpoints, SwiGLU, layer norm
 # ------------------------------------------------------------------------------------------------------------
+# The calls below are made by the compiled module `_node`, which checks the tensors' types, shapes, strides and devices (RuntimeError) and
+# allocates what the caller has not brought; the library's own refusals are Nvfp4Errors, as everywhere.
 SAVE_NOTHING, SAVE_INPUT, SAVE_CKPT8 = 0, 1, 2  # what a forward call keeps for its backward
-_CODE_OF = {torch.bfloat16: DT_BF16, torch.float32: DT_F32}
-_DTYPE_OF = (torch.bfloat16, torch.float32)
 
 
-def _on_its_device(call):
-    """The call with the device of its first argument current, whichever was before: kernels go to that device's current stream."""
-
-    @functools.wraps(call)
-    def on_device(first, *args, **kwargs):
-        dev = first.device
-        if dev.type == "cuda" and dev.index != torch._C._cuda_getDevice():
-            with torch.cuda.device(dev):
-                return call(first, *args, **kwargs)
-        return call(first, *args, **kwargs)
-
-    return on_device
-
-
-def _refuse(where: str, what: str):
-    raise RuntimeError(f"{where}: {what}")
-
-
-def _rows_of(where: str, name: str, t: torch.Tensor, shape, dtypes, device) -> int:
-    """Leading dimension of a matrix argument. What the library cannot see of a pointer is checked here: type, shape, strides and device."""
-    if t.dtype not in dtypes:
-        _refuse(where, f"{name} is {t.dtype}, not {' or '.join(str(d) for d in dtypes)}")
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        _refuse(where, f"{name} has shape {tuple(t.shape)}" + ("" if shape is None else f", not {tuple(shape)}"))
-    if t.device != device or not t.is_cuda:
-        _refuse(where, f"{name} is on {t.device}, not on {device if device.type == 'cuda' else 'a CUDA device'}")
-    rows, cols = t.shape
-    if t.stride(1) != 1 and cols > 1:
-        _refuse(where, f"{name} has columns at a stride of {t.stride(1)}")
-    return t.stride(0) if rows > 1 else (cols + 7) // 8 * 8  # (a single row's stride says nothing)
-
-
-def _vector(where: str, name: str, t: torch.Tensor, n: int, dtypes, device) -> int:
-    if t.dtype not in dtypes or t.dim() != 1 or t.numel() != n or t.device != device or (n > 1 and t.stride(0) != 1):
-        _refuse(where, f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}, not a contiguous {' or '.join(str(d) for d in dtypes)} vector of {n} on {device}")
-    return t.data_ptr()
-
-
-@_on_its_device
 def nvfp4_gemv(X: torch.Tensor, W: Operand, c_dtype: int = DT_BF16, bias: torch.Tensor | None = None, index: tuple | None = None,
                W_out: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """X [tokens, D] times quantized weights, for few tokens: X stays BF16. With outlier channels, `index` starts with (outlier columns, kept
     columns) and W_out holds their weights (Saved.W_out)."""
-    dev = X.device
-    ldx = _rows_of("nvfp4_gemv", "X", X, None, (torch.bfloat16,), dev)
-    M, D = X.shape
-    if out is None:
-        out = _matrix(M, W.R, c_dtype, dev)
-    if c_dtype not in (DT_BF16, DT_F32):
-        _check(4, "nvfp4_gemv")
-    ldy = _rows_of("nvfp4_gemv", "out", out, (M, W.R), (_DTYPE_OF[c_dtype],), dev)
-    if W.codes.device != dev or W.sf.device != dev or W.gscale.device != dev:
-        _refuse("nvfp4_gemv", f"the weights are on {W.codes.device}, X on {dev}")
-    if W.R > 0 and W.K > 0:
-        n_codes, n_sf, n_gs = _operand_sizes(W.R, W.K, W.gs_mode, W.sf_layout)
-        if W.codes.numel() < n_codes or W.sf.numel() < n_sf or W.gscale.numel() < n_gs:
-            _refuse("nvfp4_gemv", f"the weights' buffers are too small for an operand [{W.R}, {W.K}]")
-    pb = None if bias is None else _vector("nvfp4_gemv", "bias", bias, W.R, (torch.bfloat16,), dev)
-    n_out, keep, outl, wo = 0, None, None, None
-    if index is not None and index[0].numel() > 0:
-        n_out = index[0].numel()
-        outl = _vector("nvfp4_gemv", "outlier columns", index[0], n_out, (torch.int32,), dev)
-        keep = _vector("nvfp4_gemv", "kept columns", index[1], W.K, (torch.int32,), dev)
-        Kh = _lib.nvfp4_outlier_pad(n_out)
-        if W_out is None or _rows_of("nvfp4_gemv", "W_out", W_out, (W.R, Kh), (torch.bfloat16,), dev) != Kh:
-            _refuse("nvfp4_gemv", f"W_out is no contiguous [{W.R}, {Kh}]")
-        wo = W_out.data_ptr()
-    _check(_lib.nvfp4_gemv(X.data_ptr(), ldx, M, D, ctypes.byref(W.c()), keep, outl, n_out, wo, pb, out.data_ptr(), c_dtype, ldy, _stream_ptr()),
-           "nvfp4_gemv")
-    return out
+    outl, keep = (None, None) if index is None else (index[0], index[1])
+    return _node.gemv(X, W.codes, W.sf, W.gscale, W.R, W.K, W.gs_mode, W.sf_layout, c_dtype, bias, outl, keep, W_out, out)
 
 
-@dataclass
+@dataclass(slots=True)
 class Ckpt8:
     """Device buffer of an activation checkpoint in 8 bits (nvfp4_ckpt8 in the header): the codes, then the scales."""
 
@@ -924,11 +870,7 @@ class Ckpt8:
 
     @property
     def ld(self) -> int:
-        return (self.K + 31) // 32 * 32
-
-    @property
-    def device(self) -> torch.device:
-        return self.buf.device
+        return _lib.nvfp4_ckpt8_ld(self.K)
 
     @property
     def codes(self) -> torch.Tensor:
@@ -938,51 +880,29 @@ class Ckpt8:
     def scales(self) -> torch.Tensor:
         return self.buf[self.R * self.ld:].view(self.R, self.ld // 32)
 
-    def c(self) -> CCkpt8:
-        p = self.buf.data_ptr()
-        return CCkpt8(p, p + self.R * self.ld, self.R, self.K)
-
 
 def alloc_ckpt8(R: int, K: int, device="cuda") -> Ckpt8:
     """A checkpoint for a library call to fill (it writes every byte)."""
-    ld = (K + 31) // 32 * 32
+    ld = _lib.nvfp4_ckpt8_ld(K)
     return Ckpt8(torch.empty(R * (ld + ld // 32), dtype=torch.uint8, device=device), R, K)
 
 
-def _ckpt8_ref(where: str, ck: Ckpt8, R: int, K: int, device):
-    if ck.buf.dtype != torch.uint8 or not ck.buf.is_contiguous() or ck.buf.numel() != R * ck.ld * 33 // 32 or ck.R != R or ck.K != K or ck.buf.device != device:
-        _refuse(where, f"a checkpoint [{ck.R}, {ck.K}] on {ck.buf.device} for a matrix [{R}, {K}] on {device}")
-    return ctypes.byref(ck.c())
-
-
-@_on_its_device
 def nvfp4_ckpt8_pack(X: torch.Tensor, out: Ckpt8 | None = None) -> Ckpt8:
     """X (BF16 or FP32) in 8 bits."""
-    dev = X.device
-    ldx = _rows_of("nvfp4_ckpt8_pack", "X", X, None, _DTYPE_OF, dev)
-    R, K = X.shape
     if out is None:
-        out = alloc_ckpt8(R, K, dev)
-    _check(_lib.nvfp4_ckpt8_pack(X.data_ptr(), _CODE_OF[X.dtype], ldx, R, K, _ckpt8_ref("nvfp4_ckpt8_pack", out, R, K, dev), _stream_ptr()),
-           "nvfp4_ckpt8_pack")
+        return Ckpt8(_node.ckpt8_pack(X, None), *X.shape)
+    if (out.R, out.K) != tuple(X.shape):
+        raise RuntimeError(f"nvfp4_ckpt8_pack: a checkpoint of shape {(out.R, out.K)} for a matrix {tuple(X.shape)}")
+    _node.ckpt8_pack(X, out.buf)
     return out
 
 
-@_on_its_device
 def nvfp4_ckpt8_unpack(ck: Ckpt8, c_dtype: int = DT_BF16, out: torch.Tensor | None = None) -> torch.Tensor:
     """The values that a checkpoint holds (exact in either type)."""
-    dev = ck.buf.device
-    ref = _ckpt8_ref("nvfp4_ckpt8_unpack", ck, ck.R, ck.K, dev)
-    if c_dtype not in (DT_BF16, DT_F32):
-        _check(4, "nvfp4_ckpt8_unpack")
-    if out is None:
-        out = _matrix(ck.R, ck.K, c_dtype, dev)
-    ld = _rows_of("nvfp4_ckpt8_unpack", "out", out, (ck.R, ck.K), (_DTYPE_OF[c_dtype],), dev)
-    _check(_lib.nvfp4_ckpt8_unpack(ref, out.data_ptr(), c_dtype, ld, _stream_ptr()), "nvfp4_ckpt8_unpack")
-    return out
+    return _node.ckpt8_unpack(ck.buf, ck.R, ck.K, c_dtype, out)
 
 
-@dataclass
+@dataclass(slots=True)
 class SwigluSaved:
     """What nvfp4_swiglu_fwd leaves for backward: the inputs themselves, or both in 8 bits."""
 
@@ -994,47 +914,24 @@ class SwigluSaved:
     u8: Ckpt8 | None = None
 
 
-@_on_its_device
 def nvfp4_swiglu_fwd(G: torch.Tensor, U: torch.Tensor, save: int = SAVE_INPUT, out: torch.Tensor | None = None):
     """(H, saved): H = silu(G) * U; saved is None with SAVE_NOTHING."""
-    where, dev, shape, bf16 = "nvfp4_swiglu_fwd", G.device, tuple(G.shape), (torch.bfloat16,)
-    ldg, ldu = _rows_of(where, "G", G, None, bf16, dev), _rows_of(where, "U", U, shape, bf16, dev)
-    if save not in (SAVE_NOTHING, SAVE_INPUT, SAVE_CKPT8):
-        _check(4, where)
-    T, D = shape
-    H = out if out is not None else _matrix(T, D, DT_BF16, dev)
-    ldh = _rows_of(where, "out", H, shape, bf16, dev)
-    saved, r = None, (None, None)
-    if save == SAVE_INPUT:
-        saved = SwigluSaved(T, D, G, U)
-    elif save == SAVE_CKPT8:
-        saved = SwigluSaved(T, D, g8=alloc_ckpt8(T, D, dev), u8=alloc_ckpt8(T, D, dev))
-        r = (ctypes.byref(saved.g8.c()), ctypes.byref(saved.u8.c()))
-    _check(_lib.nvfp4_swiglu_fwd(G.data_ptr(), ldg, U.data_ptr(), ldu, T, D, H.data_ptr(), ldh, r[0], r[1], _stream_ptr()), where)
-    return H, saved
+    H, g8, u8 = _node.swiglu_fwd(G, U, save, out)
+    if save == SAVE_NOTHING:
+        return H, None
+    T, D = G.shape
+    return H, SwigluSaved(T, D, G, U) if g8 is None else SwigluSaved(T, D, None, None, Ckpt8(g8, T, D), Ckpt8(u8, T, D))
 
 
-@_on_its_device
 def nvfp4_swiglu_bwd(dH: torch.Tensor, saved: SwigluSaved, dG: torch.Tensor | None = None, dU: torch.Tensor | None = None):
     """(dG, dU)."""
-    where, dev, shape, bf16 = "nvfp4_swiglu_bwd", dH.device, (saved.T, saved.D), (torch.bfloat16,)
-    lddh = _rows_of(where, "dH", dH, shape, bf16, dev)
-    T, D = shape
-    p, ld, r = [None, None], [0, 0], (None, None)
-    if saved.g8 is not None:
-        r = (_ckpt8_ref(where, saved.g8, T, D, dev), _ckpt8_ref(where, saved.u8, T, D, dev))
-    else:
-        for i, (name, t) in enumerate((("G", saved.G), ("U", saved.U))):
-            p[i], ld[i] = t.data_ptr(), _rows_of(where, name, t, shape, bf16, dev)
-    dG = dG if dG is not None else _matrix(T, D, DT_BF16, dev)
-    dU = dU if dU is not None else _matrix(T, D, DT_BF16, dev)
-    lddg, lddu = _rows_of(where, "dG", dG, shape, bf16, dev), _rows_of(where, "dU", dU, shape, bf16, dev)
-    _check(_lib.nvfp4_swiglu_bwd(dH.data_ptr(), lddh, p[0], ld[0], p[1], ld[1], r[0], r[1], T, D, dG.data_ptr(), lddg, dU.data_ptr(), lddu,
-                                 _stream_ptr()), where)
-    return dG, dU
+    s, g8, u8 = saved, None, None
+    if s.g8 is not None:
+        g8, u8 = s.g8.buf, s.u8.buf
+    return _node.swiglu_bwd(dH, s.T, s.D, s.G, s.U, g8, u8, dG, dU)
 
 
-@dataclass
+@dataclass(slots=True)
 class LayerNormSaved:
     """What nvfp4_layernorm_fwd leaves for backward: mean and 1 / sqrt(variance + eps) of every row, and the input itself or in 8 bits."""
 
@@ -1048,57 +945,19 @@ class LayerNormSaved:
     x8: Ckpt8 | None = None
 
 
-@_on_its_device
 def nvfp4_layernorm_fwd(X: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor | None = None, eps: float = 1e-5, save: int = SAVE_INPUT,
                         out: torch.Tensor | None = None):
     """(Y, saved): the layer norm of X's rows (BF16 or FP32) in BF16; saved is None with SAVE_NOTHING."""
-    where, dev = "nvfp4_layernorm_fwd", X.device
-    ldx = _rows_of(where, "X", X, None, _DTYPE_OF, dev)
+    Y, stats, x8 = _node.layernorm_fwd(X, gamma, beta, eps, save, out)
+    if stats is None:
+        return Y, None
     T, D = X.shape
-    pg = _vector(where, "gamma", gamma, D, _DTYPE_OF, dev)
-    pb = None if beta is None else _vector(where, "beta", beta, D, (gamma.dtype,), dev)
-    if save not in (SAVE_NOTHING, SAVE_INPUT, SAVE_CKPT8):
-        _check(4, where)
-    Y = out if out is not None else _matrix(T, D, DT_BF16, dev)
-    ldy = _rows_of(where, "out", Y, (T, D), (torch.bfloat16,), dev)
-    x_dtype, saved, ps, r8 = _CODE_OF[X.dtype], None, None, None
-    if save != SAVE_NOTHING:
-        saved = LayerNormSaved(T, D, x_dtype, torch.empty((T, 2), dtype=torch.float32, device=dev), gamma, beta is not None)
-        ps = saved.stats.data_ptr()
-        if save == SAVE_CKPT8:
-            saved.x8 = alloc_ckpt8(T, D, dev)
-            r8 = ctypes.byref(saved.x8.c())
-        else:
-            saved.X = X
-    _check(_lib.nvfp4_layernorm_fwd(X.data_ptr(), x_dtype, ldx, T, D, pg, pb, _CODE_OF[gamma.dtype], eps, Y.data_ptr(), ldy, ps, r8, _stream_ptr()), where)
-    return Y, saved
+    return Y, LayerNormSaved(T, D, DT_F32 if X.dtype is torch.float32 else DT_BF16, stats, gamma, beta is not None, X if x8 is None else None,
+                             None if x8 is None else Ckpt8(x8, T, D))
 
 
-@_on_its_device
 def nvfp4_layernorm_bwd(dY: torch.Tensor, saved: LayerNormSaved, dX: torch.Tensor | None = None, dparam_dtype: int | None = None,
                         workspace: torch.Tensor | None = None):
     """(dX in the input's type, dgamma, dbeta): the parameters' gradients in dparam_dtype (default: gamma's); dbeta is None without beta."""
-    where, dev, T, D = "nvfp4_layernorm_bwd", dY.device, saved.T, saved.D
-    lddy = _rows_of(where, "dY", dY, (T, D), (torch.bfloat16,), dev)
-    pg = _vector(where, "gamma", saved.gamma, D, _DTYPE_OF, dev)
-    px, ldx, r8, x_type = None, 0, None, _DTYPE_OF[saved.x_dtype]
-    if saved.x8 is not None:
-        r8 = _ckpt8_ref(where, saved.x8, T, D, dev)
-    else:
-        px, ldx = saved.X.data_ptr(), _rows_of(where, "X", saved.X, (T, D), (x_type,), dev)
-    _rows_of(where, "stats", saved.stats, (T, 2), (torch.float32,), dev)
-    if not saved.stats.is_contiguous():
-        _refuse(where, "stats is not contiguous")
-    dX = dX if dX is not None else _matrix(T, D, saved.x_dtype, dev)
-    lddx = _rows_of(where, "dX", dX, (T, D), (x_type,), dev)
-    dp = _CODE_OF[saved.gamma.dtype] if dparam_dtype is None else dparam_dtype
-    if dp not in (DT_BF16, DT_F32):
-        _check(4, where)
-    dgamma = torch.empty(D, dtype=_DTYPE_OF[dp], device=dev)
-    dbeta = torch.empty(D, dtype=_DTYPE_OF[dp], device=dev) if saved.has_beta else None
-    ws = workspace if workspace is not None else _workspace(_lib.nvfp4_layernorm_bwd_workspace_bytes(T, D), dev)
-    if ws.device != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
-        _refuse(where, f"the workspace is {ws.dtype} on {ws.device}, not contiguous bytes on {dev}")
-    _check(_lib.nvfp4_layernorm_bwd(dY.data_ptr(), lddy, px, saved.x_dtype, ldx, r8, T, D, pg, _CODE_OF[saved.gamma.dtype], saved.stats.data_ptr(),
-                                    dX.data_ptr(), lddx, dgamma.data_ptr(), _ptr(dbeta), dp, ws.data_ptr(), ws.numel(), _stream_ptr()), where)
-    return dX, dgamma, dbeta
+    s = saved
+    return _node.layernorm_bwd(dY, s.T, s.D, s.x_dtype, s.X, None if s.x8 is None else s.x8.buf, s.stats, s.gamma, s.has_beta, dX, dparam_dtype, workspace)

@@ -13,9 +13,11 @@ SOURCES = ["api.cu", "quantize.cu", "gemm.cu", "hp.cu", "noalloc.cu", "calib.cu"
 # measurement aids (the tensor-core issue loop): a library of their own, loaded by the benchmark only
 MEASURE_LIB = os.path.join(HERE, "libnvfp4_measure.so")
 MEASURE_SOURCES = ["probe.cu"]
-# the autograd node of NVFP4Linear: a Python module that calls the library (found beside it) between torch's allocator and engine
+# the autograd node of NVFP4Linear and the calls around the linears: a Python module that calls the library (found beside it) between torch's
+# allocator and engine
 NODE_LIB = os.path.join(HERE, "_node.so")
-NODE_SOURCES = ["torch_node.cpp"]
+NODE_SOURCES = ["torch_node.cpp", "torch_calls.cpp"]
+NODE_HEADERS = ["torch_common.h"]
 HEADERS = ["nvfp4_device.cuh", "act8.cuh", "nvfp4_internal.h", "nvfp4_tc.cuh", os.path.join("..", "..", "include", "nvfp4.h"),
            os.path.join("..", "..", "include", "nvfp4_measure.h")]
 NVCC_FLAGS = [
@@ -47,7 +49,7 @@ def node_tag() -> str:
 
 
 def _node_stale(lib, sources) -> bool:
-    if _stale(lib, sources):
+    if _stale(lib, sources + NODE_HEADERS):
         return True
     with open(lib, "rb") as f:
         return node_tag().encode() + b"\0" not in f.read()  # (the module holds it as `built_for`)

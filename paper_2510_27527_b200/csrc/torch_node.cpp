@@ -21,13 +21,28 @@
 #include <cstring>
 #include <list>
 
-#include "../../include/nvfp4.h"
+#include "torch_common.h"
+
+using nvfp4_torch::matrix;
+using nvfp4_torch::raise_status;
+using nvfp4_torch::up;
+
+[[noreturn]] void nvfp4_torch::raise_status(nvfp4_status status, const char* where) {
+  pybind11::gil_scoped_acquire gil;
+  try {
+    pybind11::object type = pybind11::module_::import("paper_2510_27527_b200.binding").attr("Nvfp4Error");
+    PyErr_SetObject(type.ptr(), type((int)status, where).ptr());
+  } catch (pybind11::error_already_set& e) {
+    e.restore();
+  }
+  python_error e;
+  e.persist();
+  throw e;
+}
 
 namespace {
 
 using torch::autograd::variable_list;
-
-constexpr int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // The calling thread's second stream and events for calls on `stream`, made on first use. A thread enqueues its calls on one stream one
 // after another, so they share a set: a call's waits refer to the records before them in host order, and recording an event again does
@@ -61,29 +76,6 @@ void set_side(nvfp4_layer_cfg& c, c10::cuda::CUDAStream main) {
   c.ev_fork = s.events[0];
   c.ev_join = s.events[1];
   c.ev_aux = s.events[2];
-}
-
-// Row-major BF16 matrix whose rows start on 16-byte boundaries. (Not a tracked view of its buffer: a result of its own.)
-at::Tensor matrix(int64_t rows, int64_t cols, const at::TensorOptions& opt) {
-  const int64_t ld = up(cols, 8);
-  at::Tensor t = at::empty({rows, ld}, opt);
-  if (ld == cols) return t;
-  at::AutoDispatchBelowADInplaceOrView below;
-  return t.narrow(1, 0, cols);
-}
-
-// Status of a library call, as the exception that the binding raises for it.
-[[noreturn]] void raise_status(nvfp4_status status, const char* where) {
-  pybind11::gil_scoped_acquire gil;
-  try {
-    pybind11::object type = pybind11::module_::import("paper_2510_27527_b200.binding").attr("Nvfp4Error");
-    PyErr_SetObject(type.ptr(), type((int)status, where).ptr());
-  } catch (pybind11::error_already_set& e) {
-    e.restore();
-  }
-  python_error e;
-  e.persist();
-  throw e;
 }
 
 // What a call is beside its tensors.
@@ -310,7 +302,7 @@ PyMODINIT_FUNC PyInit__node() {
            PyUnicode_InternFromString("outlier_fp8"), PyUnicode_InternFromString("w_block16"), PyUnicode_InternFromString("concurrent"),
            PyUnicode_InternFromString("dev_status")};
   PyObject* module = PyModule_Create(&module_def);
-  if (module && PyModule_AddStringConstant(module, "built_for", NODE_TAG) < 0) {
+  if (module && (PyModule_AddStringConstant(module, "built_for", NODE_TAG) < 0 || PyModule_AddFunctions(module, nvfp4_torch::block_methods) < 0)) {
     Py_DECREF(module);
     return nullptr;
   }

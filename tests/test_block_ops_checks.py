@@ -91,7 +91,7 @@ def test_the_binding_refuses_what_the_library_cannot_see():
     for call in on_cpu:
         with pytest.raises(RuntimeError, match="CUDA device"):
             call()
-    with pytest.raises(RuntimeError, match="float16"):
+    with pytest.raises(RuntimeError, match="Half"):
         b.nvfp4_layernorm_fwd(x.half(), v)
     with pytest.raises(RuntimeError, match="shape"):
         b.nvfp4_swiglu_fwd(x[0], x[0])
