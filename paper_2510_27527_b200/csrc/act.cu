@@ -17,37 +17,67 @@ __device__ __forceinline__ int64_t quotient(int64_t n, int64_t d, int64_t total)
   return total <= 0xFFFFFFFFll ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d;
 }
 
-template <int SRC>
+// NB pieces of eight elements a thread, one CTA's next to one another: one piece's loads of all threads of an SM (32 KB from BF16, 16 KB of
+// codes) are fewer than memory needs in flight.
+template <int SRC, int NB>
 __global__ void __launch_bounds__(256) ckpt8_pack_kernel(ActSrc x, int64_t R, int D, int ldc, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
   pdl_prologue();
   const int64_t n8 = ldc >> 3, total = R * n8;
-  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x;  // (a group's four threads are in one warp: n8 is a multiple of 4)
-  const bool live = gid < total;
-  const int64_t row = live ? quotient(gid, n8, total) : 0;
-  const int c = (int)(gid - row * n8) << 3;
-  float v[8] = {};
-  if (live && c < D) values8(load8<SRC>(x, row, c, D), v);
-  ckpt8_store(v, codes + row * ldc, scales + row * (ldc >> 5), c, live);
+  const int64_t first = (int64_t)blockIdx.x * (256 * NB) + threadIdx.x;  // (a group's four threads are in one warp: n8 is a multiple of 4)
+  Raw8<SRC> r[NB];
+  int64_t row[NB];
+  int c[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const int64_t gid = first + j * 256;
+    row[j] = gid < total ? quotient(gid, n8, total) : 0;
+    c[j] = (int)(gid - row[j] * n8) << 3;
+    r[j] = Raw8<SRC>{};
+    if (gid < total && c[j] < D) r[j] = load8<SRC>(x, row[j], c[j], D);
+  }
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    f32x2 v[4];
+    values8(r[j], v);
+    ckpt8_store(v, amax8(r[j]), codes + row[j] * ldc, scales + row[j] * (ldc >> 5), c[j], first + j * 256 < total);
+  }
 }
 
-template <bool F32>
+template <bool F32, int NB>
 __global__ void __launch_bounds__(256) ckpt8_unpack_kernel(ActSrc x, int64_t R, int D, void* __restrict__ out, int64_t ld) {
   pdl_prologue();
   const int64_t n8 = (D + 7) >> 3, total = R * n8;
-  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (gid >= total) return;
-  const int64_t row = quotient(gid, n8, total);
-  const int c = (int)(gid - row * n8) << 3;
-  float v[8];
-  values8(load8<kSrcCkpt8>(x, row, c, D), v);
-  if (F32)
-    store_f32x8(static_cast<float*>(out) + row * ld, c, D, v);
-  else
-    store_bf16x8(static_cast<uint16_t*>(out) + row * ld, c, D, v);
+  const int64_t first = (int64_t)blockIdx.x * (256 * NB) + threadIdx.x;
+  Raw8<kSrcCkpt8> r[NB];
+  int64_t row[NB];
+  int c[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const int64_t gid = first + j * 256;
+    if (gid >= total) break;
+    row[j] = quotient(gid, n8, total);
+    c[j] = (int)(gid - row[j] * n8) << 3;
+    r[j] = load8<kSrcCkpt8>(x, row[j], c[j], D);
+  }
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    if (first + j * 256 >= total) break;
+    f32x2 v[4];
+    values8(r[j], v);
+    if (F32)
+      store_f32x8(static_cast<float*>(out) + row[j] * ld, c[j], D, v);
+    else
+      store_bf16x8(static_cast<uint16_t*>(out) + row[j] * ld, c[j], D, v);
+  }
 }
 
 // 1 / (1 + exp(-g)): 1 at +inf, 0 at -inf
 __device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
+
+__device__ __forceinline__ f32x2 sigmoid2(f32x2 g) {
+  const float2 v = values_of(g);
+  return pair_of(sigmoid(v.x), sigmoid(v.y));
+}
 
 struct CkptOut {
   uint8_t *codes, *scales;
@@ -61,19 +91,23 @@ __global__ void __launch_bounds__(256) swiglu_fwd_kernel(ActSrc g, ActSrc u, int
   const bool live = gid < total;
   const int64_t row = live ? quotient(gid, n8, total) : 0;
   const int c = (int)(gid - row * n8) << 3;
-  float gv[8] = {}, uv[8] = {};
+  Raw8<kSrcBf16> gr{}, ur{};
   if (live && c < D) {
-    const Raw8<kSrcBf16> gr = load8<kSrcBf16>(g, row, c, D), ur = load8<kSrcBf16>(u, row, c, D);
-    values8(gr, gv);
-    values8(ur, uv);
-    float o[8];
+    gr = load8<kSrcBf16>(g, row, c, D);
+    ur = load8<kSrcBf16>(u, row, c, D);
+  }
+  f32x2 gv[4], uv[4];
+  values8(gr, gv);
+  values8(ur, uv);
+  if (live && c < D) {
+    f32x2 o[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = gv[i] * sigmoid(gv[i]) * uv[i];
+    for (int i = 0; i < 4; ++i) o[i] = mul2(mul2(gv[i], sigmoid2(gv[i])), uv[i]);
     store_bf16x8(h + row * ldh, c, D, o);
   }
   if (CK) {
-    ckpt8_store(gv, cg.codes + row * ldc, cg.scales + row * (ldc >> 5), c, live);
-    ckpt8_store(uv, cu.codes + row * ldc, cu.scales + row * (ldc >> 5), c, live);
+    ckpt8_store(gv, amax8(gr), cg.codes + row * ldc, cg.scales + row * (ldc >> 5), c, live);
+    ckpt8_store(uv, amax8(ur), cu.codes + row * ldc, cu.scales + row * (ldc >> 5), c, live);
   }
 }
 
@@ -88,26 +122,28 @@ __global__ void __launch_bounds__(256) swiglu_bwd_kernel(ActSrc dh, ActSrc g, Ac
   const int c = (int)(gid - row * n8) << 3;
   const Raw8<kSrcBf16> hr = load8<kSrcBf16>(dh, row, c, D);
   const Raw8<SRC> gr = load8<SRC>(g, row, c, D), ur = load8<SRC>(u, row, c, D);
-  float hv[8], gv[8], uv[8], a[8], b[8];
+  f32x2 hv[4], gv[4], uv[4], a[4], b[4];
   values8(hr, hv);
   values8(gr, gv);
   values8(ur, uv);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float s = sigmoid(gv[i]);
-    a[i] = hv[i] * uv[i] * (s * (1.0f + gv[i] * (1.0f - s)));
-    b[i] = hv[i] * (gv[i] * s);
+  for (int i = 0; i < 4; ++i) {
+    const f32x2 s = sigmoid2(gv[i]), one = pair_of(1.0f), rest = fma2(s, pair_of(-1.0f), one);
+    a[i] = mul2(mul2(hv[i], uv[i]), mul2(s, fma2(gv[i], rest, one)));
+    b[i] = mul2(hv[i], mul2(gv[i], s));
   }
   store_bf16x8(dg + row * lddg, c, D, a);
   store_bf16x8(du + row * lddu, c, D, b);
 }
 
 constexpr int64_t kMaxCols = (int64_t)1 << 24;  // columns are 32-bit in the kernels
-// CTAs of 256 threads for `threads` threads, 0: more than a grid has
-unsigned ctas(int64_t threads) {
-  const int64_t n = (threads + 255) / 256;
+// CTAs of 256 threads for `pieces` pieces, nb a thread; 0: more than a grid has
+unsigned ctas(int64_t pieces, int nb = 1) {
+  const int64_t n = (pieces + 256 * nb - 1) / (256 * nb);
   return n <= 0x7FFFFFFF ? (unsigned)n : 0u;
 }
+// Up to here a call's pieces are all in flight at once, one a thread.
+int64_t few_pieces() { return (int64_t)device_sm_count() * 2048; }
 nvfp4_status launched() { return cudaGetLastError() == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA; }
 
 }  // namespace
@@ -139,12 +175,16 @@ nvfp4_status nvfp4_ckpt8_pack(const void* X, int32_t x_dtype, int64_t ldx, int64
   if (!X) return NVFP4_ERR_NULL;
   if (bad_matrix(X, ldx, K, x_dtype == NVFP4_DT_F32 ? 4 : 2)) return NVFP4_ERR_ALIGN;
   const int64_t ldc = nvfp4_ckpt8_ld(K);
-  const unsigned grid = ctas(R * (ldc / 8));
+  const int64_t pieces = R * (ldc / 8);
+  const int nb = pieces > few_pieces() ? 2 : 1;
+  const unsigned grid = ctas(pieces, nb);
   if (!grid) return NVFP4_ERR_LIMIT;
   if (!device_is_sm100()) return NVFP4_ERR_ARCH;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const ActSrc x{X, nullptr, ldx};
-  launch_kernel(x_dtype == NVFP4_DT_F32 ? ckpt8_pack_kernel<kSrcF32> : ckpt8_pack_kernel<kSrcBf16>, dim3(grid), dim3(256), 0, st, x, R, (int)K, (int)ldc, out->codes, out->scales);
+  const bool f32 = x_dtype == NVFP4_DT_F32;
+  auto kernel = nb == 1 ? (f32 ? ckpt8_pack_kernel<kSrcF32, 1> : ckpt8_pack_kernel<kSrcBf16, 1>) : (f32 ? ckpt8_pack_kernel<kSrcF32, 2> : ckpt8_pack_kernel<kSrcBf16, 2>);
+  launch_kernel(kernel, dim3(grid), dim3(256), 0, st, x, R, (int)K, (int)ldc, out->codes, out->scales);
   return launched();
 }
 
@@ -158,12 +198,16 @@ nvfp4_status nvfp4_ckpt8_unpack(const nvfp4_ckpt8* in, void* X, int32_t x_dtype,
   if (in->R == 0) return NVFP4_OK;
   if (!X) return NVFP4_ERR_NULL;
   if (bad_matrix(X, ldx, in->K, x_dtype == NVFP4_DT_F32 ? 4 : 2)) return NVFP4_ERR_ALIGN;
-  const unsigned grid = ctas(in->R * ((in->K + 7) / 8));
+  const int64_t pieces = in->R * ((in->K + 7) / 8);
+  const int nb = pieces > few_pieces() ? 4 : 1;
+  const unsigned grid = ctas(pieces, nb);
   if (!grid) return NVFP4_ERR_LIMIT;
   if (!device_is_sm100()) return NVFP4_ERR_ARCH;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const ActSrc x{in->codes, in->scales, nvfp4_ckpt8_ld(in->K)};
-  launch_kernel(x_dtype == NVFP4_DT_F32 ? ckpt8_unpack_kernel<true> : ckpt8_unpack_kernel<false>, dim3(grid), dim3(256), 0, st, x, in->R, (int)in->K, X, ldx);
+  const bool f32 = x_dtype == NVFP4_DT_F32;
+  auto kernel = nb == 1 ? (f32 ? ckpt8_unpack_kernel<true, 1> : ckpt8_unpack_kernel<false, 1>) : (f32 ? ckpt8_unpack_kernel<true, 4> : ckpt8_unpack_kernel<false, 4>);
+  launch_kernel(kernel, dim3(grid), dim3(256), 0, st, x, in->R, (int)in->K, X, ldx);
   return launched();
 }
 

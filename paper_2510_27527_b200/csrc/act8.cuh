@@ -13,6 +13,40 @@ nvfp4_status check_ckpt8(const nvfp4_ckpt8* c, int64_t R, int64_t K);  // a chec
 
 constexpr int kSrcBf16 = 0, kSrcF32 = 1, kSrcCkpt8 = 2;
 
+// Two binary32 values in a register pair; one packed instruction each. The kernels around the linears issue about as many instructions as
+// they have time for beside memory, and most of them are such.
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pair_of(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ f32x2 pair_of(float v) { return pair_of(v, v); }
+__device__ __forceinline__ float2 values_of(f32x2 p) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ float sum_of(f32x2 p) {
+  const float2 v = values_of(p);
+  return v.x + v.y;
+}
+
 // ---------------------------------------------------------------------------------------------------------
 // the checkpoint's format
 // ---------------------------------------------------------------------------------------------------------
@@ -27,39 +61,56 @@ __device__ __forceinline__ uint32_t ckpt8_scale_byte(float a) {
 __device__ __forceinline__ float ckpt8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }            // byte in 10 .. 247
 __device__ __forceinline__ float ckpt8_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }  // 1 / scale, exactly
 
-// The eight codes of v at a group's scale (the product is exact unless it lies far below the smallest code), lowest element first.
-__device__ __forceinline__ uint2 ckpt8_encode(const float (&v)[8], float inverse) {
+// The eight codes of v at a group's scale (the product is exact unless it lies far below the smallest code), lowest element first. NaN has
+// a code of its own, infinities would saturate.
+__device__ __forceinline__ uint2 ckpt8_encode(const f32x2 (&v)[4], float inverse) {
   uint16_t h[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h[i]) : "f"(__fmul_rn(v[2 * i + 1], inverse)), "f"(__fmul_rn(v[2 * i], inverse)));
+  for (int i = 0; i < 4; ++i) {
+    const float2 y = values_of(mul2(v[i], pair_of(inverse)));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h[i]) : "f"(y.y), "f"(y.x));
+  }
   return make_uint2((uint32_t)h[0] | (uint32_t)h[1] << 16, (uint32_t)h[2] | (uint32_t)h[3] << 16);
 }
-__device__ __forceinline__ void ckpt8_decode(const uint2& q, float scale, float (&v)[8]) {  // exact
+// The codes' own values, without the group's scale.
+__device__ __forceinline__ void ckpt8_decode(const uint2& q, f32x2 (&v)[4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t w = i < 2 ? q.x : q.y;
     uint32_t h2;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"((uint16_t)((i & 1) ? w >> 16 : w & 0xFFFFu)));
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h2));
-    v[2 * i] = __fmul_rn(f.x, scale);
-    v[2 * i + 1] = __fmul_rn(f.y, scale);
+    v[i] = pair_of(f.x, f.y);
   }
 }
-// Stores the checkpoint of the eight elements v at column c of a row (c < ld, a multiple of 8; elements past the row's end are 0).
-// All four threads of a group call this together, whether they have elements or not; `store` says whether this one writes.
-__device__ __forceinline__ void ckpt8_store(const float (&x)[8], uint8_t* codes_row, uint8_t* scales_row, int c, bool store) {
-  float v[8], a = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    v[i] = finite_or_nan(x[i]);
-    a = fmaxf(a, fabsf(v[i]));  // (the maximum of a number and NaN is the number)
-  }
+// Stores the checkpoint of the eight elements v, whose largest finite-or-infinite magnitude is a, at column c of a row (c < ld, a multiple of
+// 8; elements past the row's end are 0). All four threads of a group call this together, whether they have elements or not; `store` says
+// whether this one writes.
+__device__ __forceinline__ void ckpt8_store(const f32x2 (&v)[4], float a, uint8_t* codes_row, uint8_t* scales_row, int c, bool store) {
+  a = fmaxf(a, 0.0f);  // (only NaN: 0)
   a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
   a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
-  const uint32_t byte = ckpt8_scale_byte(a);
+  uint32_t byte = ckpt8_scale_byte(a);
+  uint2 q;
+  if (__any_sync(0xFFFFFFFFu, a == __uint_as_float(0x7F800000u))) {  // an infinity in one of the warp's groups: it becomes NaN and does not count
+    f32x2 u[4];
+    a = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = values_of(v[i]);
+      const float lo = finite_or_nan(f.x), hi = finite_or_nan(f.y);
+      a = fmaxf(a, fmaxf(fabsf(lo), fabsf(hi)));  // (the maximum of a number and NaN is the number)
+      u[i] = pair_of(lo, hi);
+    }
+    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
+    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
+    byte = ckpt8_scale_byte(a);
+    q = ckpt8_encode(u, ckpt8_inverse(byte));
+  } else {
+    q = ckpt8_encode(v, ckpt8_inverse(byte));
+  }
   if (!store) return;
-  *reinterpret_cast<uint2*>(codes_row + c) = ckpt8_encode(v, ckpt8_inverse(byte));
+  *reinterpret_cast<uint2*>(codes_row + c) = q;
   if ((c & 31) == 0) scales_row[c >> 5] = (uint8_t)byte;
 }
 
@@ -82,18 +133,33 @@ struct Raw8<kSrcCkpt8> {
   float scale;
 };
 
-__device__ __forceinline__ void bf16x8_values(const uint4& w, float (&v)[8]) {
-  v[0] = bf16_lo(w.x); v[1] = bf16_hi(w.x);
-  v[2] = bf16_lo(w.y); v[3] = bf16_hi(w.y);
-  v[4] = bf16_lo(w.z); v[5] = bf16_hi(w.z);
-  v[6] = bf16_lo(w.w); v[7] = bf16_hi(w.w);
+__device__ __forceinline__ f32x2 bf16_pair(uint32_t w) { return pair_of(bf16_lo(w), bf16_hi(w)); }
+__device__ __forceinline__ void values8(const Raw8<kSrcBf16>& r, f32x2 (&v)[4]) {
+  v[0] = bf16_pair(r.w.x);
+  v[1] = bf16_pair(r.w.y);
+  v[2] = bf16_pair(r.w.z);
+  v[3] = bf16_pair(r.w.w);
 }
-__device__ __forceinline__ void values8(const Raw8<kSrcBf16>& r, float (&v)[8]) { bf16x8_values(r.w, v); }
-__device__ __forceinline__ void values8(const Raw8<kSrcF32>& r, float (&v)[8]) {
-  v[0] = r.lo.x; v[1] = r.lo.y; v[2] = r.lo.z; v[3] = r.lo.w;
-  v[4] = r.hi.x; v[5] = r.hi.y; v[6] = r.hi.z; v[7] = r.hi.w;
+__device__ __forceinline__ void values8(const Raw8<kSrcF32>& r, f32x2 (&v)[4]) {
+  v[0] = pair_of(r.lo.x, r.lo.y);
+  v[1] = pair_of(r.lo.z, r.lo.w);
+  v[2] = pair_of(r.hi.x, r.hi.y);
+  v[3] = pair_of(r.hi.z, r.hi.w);
 }
-__device__ __forceinline__ void values8(const Raw8<kSrcCkpt8>& r, float (&v)[8]) { ckpt8_decode(r.q, r.scale, v); }
+__device__ __forceinline__ void values8(const Raw8<kSrcCkpt8>& r, f32x2 (&v)[4]) {  // exact
+  ckpt8_decode(r.q, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], pair_of(r.scale));
+}
+// The largest magnitude of the eight, NaN left out (NaN where there is nothing else).
+__device__ __forceinline__ float amax8(const Raw8<kSrcBf16>& r) {
+  const uint32_t m = amax16x2(amax16x2(r.w.x, r.w.y), amax16x2(r.w.z, r.w.w));
+  return fmaxf(fabsf(bf16_lo(m)), fabsf(bf16_hi(m)));
+}
+__device__ __forceinline__ float amax8(const Raw8<kSrcF32>& r) {
+  return fmaxf(fmaxf(fmaxf(fabsf(r.lo.x), fabsf(r.lo.y)), fmaxf(fabsf(r.lo.z), fabsf(r.lo.w))),
+               fmaxf(fmaxf(fabsf(r.hi.x), fabsf(r.hi.y)), fmaxf(fabsf(r.hi.z), fabsf(r.hi.w))));
+}
 
 // Elements c .. c + 7 of a row of D (c a multiple of 8; the row starts on a 16-byte boundary). Elements from D on are 0 and not read.
 __device__ __forceinline__ uint4 load_bf16x8(const uint16_t* row, int c, int D) {
@@ -142,26 +208,31 @@ __device__ __forceinline__ uint32_t bf16x2_of(float lo, float hi) {
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
   return w;
 }
-__device__ __forceinline__ void store_bf16x8(uint16_t* row, int c, int D, const float (&v)[8]) {
-  const uint4 w = make_uint4(bf16x2_of(v[0], v[1]), bf16x2_of(v[2], v[3]), bf16x2_of(v[4], v[5]), bf16x2_of(v[6], v[7]));
-  if (c + 8 <= D) {
-    *reinterpret_cast<uint4*>(row + c) = w;
-    return;
-  }
-  const uint32_t h[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (c + i < D) row[c + i] = (uint16_t)(h[i >> 1] >> (16 * (i & 1)));
+__device__ __forceinline__ uint32_t bf16x2_of(f32x2 p) {
+  const float2 v = values_of(p);
+  return bf16x2_of(v.x, v.y);
 }
-__device__ __forceinline__ void store_f32x8(float* row, int c, int D, const float (&v)[8]) {
+__device__ __forceinline__ void store_bf16x8(uint16_t* row, int c, int D, const f32x2 (&v)[4]) {
+  const uint32_t w[4] = {bf16x2_of(v[0]), bf16x2_of(v[1]), bf16x2_of(v[2]), bf16x2_of(v[3])};
   if (c + 8 <= D) {
-    *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4*>(row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    *reinterpret_cast<uint4*>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
     return;
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (c + i < D) row[c + i] = v[i];
+    if (c + i < D) row[c + i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+}
+__device__ __forceinline__ void store_f32x8(float* row, int c, int D, const f32x2 (&v)[4]) {
+  const float2 a = values_of(v[0]), b = values_of(v[1]), d = values_of(v[2]), e = values_of(v[3]);
+  if (c + 8 <= D) {
+    *reinterpret_cast<float4*>(row + c) = make_float4(a.x, a.y, b.x, b.y);
+    *reinterpret_cast<float4*>(row + c + 4) = make_float4(d.x, d.y, e.x, e.y);
+    return;
+  }
+  const float f[8] = {a.x, a.y, b.x, b.y, d.x, d.y, e.x, e.y};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (c + i < D) row[c + i] = f[i];
 }
 
 }  // namespace nvfp4

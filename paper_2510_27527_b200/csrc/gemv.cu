@@ -234,12 +234,12 @@ __global__ void __launch_bounds__(kThreads) gemv_kernel(GemvArgs a) {
           uint8_t* at = xs + (size_t)it[p] * 256 * Mg;
           if (s0 + it[p] < a.n_codes) {
             const float to = __uint_as_float((268u - e) << 23);  // 2^(141 - e)
-            float v[8];
-            bf16x8_values(w[p], v);
+            const uint32_t wj[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
             uint32_t h[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const __half2 q = __floats2half2_rn(v[2 * j] * to, v[2 * j + 1] * to);
+              const float2 v = values_of(mul2(bf16_pair(wj[j]), pair_of(to)));
+              const __half2 q = __floats2half2_rn(v.x, v.y);
               h[j] = *reinterpret_cast<const uint32_t*>(&q);
             }
             *reinterpret_cast<uint4*>(at + (((l16 & 3) * Mg + m[p]) * 4 + (l16 >> 2)) * 16) = make_uint4(h[0], h[1], h[2], h[3]);

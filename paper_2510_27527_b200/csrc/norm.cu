@@ -1,9 +1,10 @@
 // Layer norm over the rows of x [T, D], the step in front of a block's linears:
 //   forward   m = mean(x), v = mean((x - m)^2), r = 1 / sqrt(v + eps), y = (x - m) r gamma + beta, optionally with the checkpoint of x
 //   backward  xh = (x - m) r, h = dy gamma:  dx = r (h - mean(h) - xh mean(h xh)),  dgamma = sum_t dy xh,  dbeta = sum_t dy
-// with x itself or its 8-bit checkpoint in backward. One pass over memory each: a group of TPR threads holds a whole row in registers, eight
-// neighbouring elements at a time, so that mean, centred squares and result need x once. Backward's groups walk over rows and keep the two
-// column sums of their columns in registers; the groups of a CTA add theirs up in shared memory, the CTAs through a small FP32 matrix that a
+// with x itself or its 8-bit checkpoint in backward. One pass over memory each: a group of TPR threads holds a row in registers, eight
+// neighbouring elements at a time, so that mean, centred squares and result need x once. Groups walk over rows and load the next row while they
+// work on this one; the parameters stay in registers (forward) or, as FP32, in shared memory (backward, whose registers hold the two sums of
+// the thread's columns). At the end the groups of a CTA add their column sums up in shared memory, the CTAs through a small FP32 matrix that a
 // second launch sums. Every sum has a fixed order.
 #include "../../include/nvfp4.h"
 
@@ -15,20 +16,23 @@ namespace nvfp4 {
 namespace {
 
 constexpr int kMaxD = 16384;  // TPR 512, four vectors of eight a thread
-// CTAs of backward, at most. A tuning constant, not a hardware query: the workspace size derived from it must not depend on the device.
-constexpr int kBwdCtas = 592;
+// CTAs, at most. Tuning constants, not hardware queries: the workspace size derived from backward's must not depend on the device.
+constexpr int kBwdCtas = 296, kFwdCtas = 888;
 
 template <int TPR>
 constexpr int kThreadsOf = TPR < 256 ? 256 : TPR;  // of a CTA
 
+template <int TPR>
+constexpr int kSlots = kThreadsOf<TPR> / 32;  // of group_sum2, one set
+
 // eight parameters from column c on, 0 past D
-__device__ __forceinline__ void params8(const void* p, int f32, int c, int D, float (&v)[8]) {
+__device__ __forceinline__ void params8(const void* p, int f32, int c, int D, f32x2 (&v)[4]) {
   if (f32) {
     Raw8<kSrcF32> r;
     load_f32x8(static_cast<const float*>(p), c, D, r.lo, r.hi);
     values8(r, v);
   } else {
-    bf16x8_values(load_bf16x8(static_cast<const uint16_t*>(p), c, D), v);
+    values8(Raw8<kSrcBf16>{load_bf16x8(static_cast<const uint16_t*>(p), c, D)}, v);
   }
 }
 
@@ -39,26 +43,42 @@ __device__ __forceinline__ void group_barrier(int group) {
   else
     asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(TPR) : "memory");
 }
-// Sums of two values over the group's threads, in all of them. `slot`: shared memory that no thread of the group may still be reading from
-// an earlier call (calls alternate between two, a barrier in each).
+// Sum over the group's threads, in all of them. `slot`: shared memory that no thread of the group may still be reading from an earlier call
+// (calls alternate between two, a barrier in each).
 template <int TPR>
-__device__ __forceinline__ float2 group_sum2(float2 v, float2* slot, int group, int lane) {
+__device__ __forceinline__ float group_sum(float v, float* slot, int group, int lane) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
-    v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
-  }
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
   if constexpr (TPR > 32) {
     if ((lane & 31) == 0) slot[lane >> 5] = v;
     group_barrier<TPR>(group);
     v = slot[0];
 #pragma unroll
-    for (int w = 1; w < TPR / 32; ++w) {
-      v.x += slot[w].x;
-      v.y += slot[w].y;
-    }
+    for (int w = 1; w < TPR / 32; ++w) v += slot[w];
   }
   return v;
+}
+// Two sums at once: the half warps exchange, so that each adds up one of the two.
+template <int TPR>
+__device__ __forceinline__ float2 group_sum2(float x, float y, float2* slot, int group, int lane) {
+  const bool upper = lane & 16;
+  float v = (upper ? y : x) + __shfl_xor_sync(0xFFFFFFFFu, upper ? x : y, 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  if constexpr (TPR > 32) {
+    if ((lane & 15) == 0) reinterpret_cast<float*>(slot)[lane >> 4] = v;
+    group_barrier<TPR>(group);
+    float2 s = slot[0];
+#pragma unroll
+    for (int w = 1; w < TPR / 32; ++w) {
+      s.x += slot[w].x;
+      s.y += slot[w].y;
+    }
+    return s;
+  } else {
+    const float other = __shfl_xor_sync(0xFFFFFFFFu, v, 16);
+    return upper ? make_float2(other, v) : make_float2(v, other);
+  }
 }
 
 struct NormFwdArgs {
@@ -77,55 +97,77 @@ template <int SRC, bool CK, int NV, int TPR>
 __global__ void __launch_bounds__(kThreadsOf<TPR>) norm_fwd_kernel(NormFwdArgs a) {
   pdl_prologue();
   constexpr int GROUPS = kThreadsOf<TPR> / TPR;
-  __shared__ float2 slots[2][GROUPS][TPR / 32];
-  const int group = threadIdx.x / TPR, lane = threadIdx.x % TPR, D = a.D;
-  const int64_t row = (int64_t)blockIdx.x * GROUPS + group;
-  if (row >= a.T) return;  // (the whole group)
-  float v[NV][8];
-  float sum = 0.0f;
-  {
-    Raw8<SRC> raw[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + lane) * 8;
-      if (c < D) raw[i] = load8<SRC>(a.x, row, c, D);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + lane) * 8;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
-      if (c < D) values8(raw[i], v[i]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum += v[i][e];
-    }
-  }
+  __shared__ float slots[2][GROUPS][TPR / 32];
+  const int group = threadIdx.x / TPR, lane = threadIdx.x % TPR, D = a.D, ldc = (D + 31) & ~31;
   const float inv_D = 1.0f / (float)D;
-  const float mean = group_sum2<TPR>(make_float2(sum, 0.0f), slots[0][group], group, lane).x * inv_D;
-  float sq = 0.0f;
+  const f32x2 minus_one = pair_of(-1.0f);
+  Raw8<SRC> next[NV];
+  auto fetch = [&](int64_t row) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (i * TPR + lane) * 8;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float d = v[i][e] - mean;
-      if (c + e < D) sq = fmaf(d, d, sq);
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * TPR + lane) * 8;
+      next[i] = Raw8<SRC>{};
+      if (c < D && row < a.T) next[i] = load8<SRC>(a.x, row, c, D);
     }
-  }
-  const float var = group_sum2<TPR>(make_float2(sq, 0.0f), slots[1][group], group, lane).x * inv_D;
-  const float rstd = 1.0f / sqrtf(var + a.eps);
-  if (a.stats && lane == 0) a.stats[row] = make_float2(mean, rstd);
-  const int ldc = (D + 31) & ~31;
+  };
+  int64_t row = (int64_t)blockIdx.x * GROUPS + group;
+  fetch(row);
+  f32x2 g[NV][4], b[NV][4];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (i * TPR + lane) * 8;
-    if (CK) ckpt8_store(v[i], a.codes + row * ldc, a.scales + row * (ldc >> 5), c, c < ldc);
-    if (c < D) {
-      float g[8], b[8] = {}, o[8];
-      params8(a.gamma, a.params_f32, c, D, g);
-      if (a.beta) params8(a.beta, a.params_f32, c, D, b);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = fmaf((v[i][e] - mean) * rstd, g[e], b[e]);
+    for (int e = 0; e < 4; ++e) g[i][e] = b[i][e] = pair_of(0.0f);
+    if (c < D) params8(a.gamma, a.params_f32, c, D, g[i]);
+    if (c < D && a.beta) params8(a.beta, a.params_f32, c, D, b[i]);
+  }
+  for (; row < a.T; row += (int64_t)gridDim.x * GROUPS) {
+    f32x2 v[NV][4];
+    float amax[NV];
+    f32x2 sum = pair_of(0.0f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      values8(next[i], v[i]);
+      if (CK) amax[i] = amax8(next[i]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum = add2(sum, v[i][e]);
+    }
+    fetch(row + (int64_t)gridDim.x * GROUPS);
+    if (CK) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + lane) * 8;
+        ckpt8_store(v[i], amax[i], a.codes + row * ldc, a.scales + row * (ldc >> 5), c, c < ldc);
+      }
+    }
+    const float mean = group_sum<TPR>(sum_of(sum), slots[0][group], group, lane) * inv_D;
+    f32x2 sq = pair_of(0.0f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * TPR + lane) * 8;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i][e] = fma2(minus_one, pair_of(mean), v[i][e]);  // x - m, rounded once
+      if (c + 8 <= D) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sq = fma2(v[i][e], v[i][e], sq);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 d = values_of(v[i][e]);
+          sq = add2(sq, pair_of(c + 2 * e < D ? d.x * d.x : 0.0f, c + 2 * e + 1 < D ? d.y * d.y : 0.0f));
+        }
+      }
+    }
+    const float var = group_sum<TPR>(sum_of(sq), slots[1][group], group, lane) * inv_D;
+    const float rstd = 1.0f / sqrtf(var + a.eps);
+    if (a.stats && lane == 0) a.stats[row] = make_float2(mean, rstd);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * TPR + lane) * 8;
+      if (c >= D) continue;
+      f32x2 o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fma2(mul2(v[i][e], pair_of(rstd)), g[i][e], b[i][e]);
       store_bf16x8(a.y + row * a.ldy, c, D, o);
     }
   }
@@ -143,60 +185,79 @@ struct NormBwdArgs {
 };
 
 template <int SRC, int NV, int TPR>
-__global__ void __launch_bounds__(kThreadsOf<TPR>) norm_bwd_kernel(NormBwdArgs a) {
+__global__ void __launch_bounds__(kThreadsOf<TPR>, TPR > 256 ? 1 : 2) norm_bwd_kernel(NormBwdArgs a) {
   pdl_prologue();
   constexpr int GROUPS = kThreadsOf<TPR> / TPR;
-  __shared__ float2 slots[2][GROUPS][TPR / 32];
-  extern __shared__ float sums[];  // GROUPS / 2 times [dgamma, dbeta][NV][8][TPR]
+  extern __shared__ __align__(16) uint8_t smem[];
   const int group = threadIdx.x / TPR, lane = threadIdx.x % TPR, D = a.D;
+  float2* const slots = reinterpret_cast<float2*>(smem) + group * (TPR / 32);  // and again kSlots further on
+  f32x2* const gamma = reinterpret_cast<f32x2*>(smem) + 2 * kSlots<TPR>;       // [NV][4][TPR]
+  f32x2* const sums = gamma;                            // and at the end, GROUPS / 2 times [dgamma, dbeta][NV][4][TPR]
   const float inv_D = 1.0f / (float)D;
-  float dg[NV][8] = {}, db[NV][8] = {};
-  int parity = 0;
-  for (int64_t row = (int64_t)blockIdx.x * GROUPS + group; row < a.T; row += (int64_t)gridDim.x * GROUPS, parity ^= 1) {
-    Raw8<kSrcBf16> dyr[NV];
-    Raw8<SRC> xr[NV];
+  Raw8<kSrcBf16> dy_next[NV];
+  Raw8<SRC> x_next[NV];
+  float2 st_next = make_float2(0.0f, 0.0f);
+  auto fetch = [&](int64_t row) {
+    if (row >= a.T) return;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + lane) * 8;
+      dy_next[i] = Raw8<kSrcBf16>{};
+      x_next[i] = Raw8<SRC>{};
       if (c < D) {
-        dyr[i] = load8<kSrcBf16>(a.dy, row, c, D);
-        xr[i] = load8<SRC>(a.x, row, c, D);
+        dy_next[i] = load8<kSrcBf16>(a.dy, row, c, D);
+        x_next[i] = load8<SRC>(a.x, row, c, D);
       }
     }
-    const float2 st = a.stats[row];
-    float2 s = make_float2(0.0f, 0.0f);
+    st_next = a.stats[row];
+  };
+  int64_t row = (int64_t)blockIdx.x * GROUPS + group;
+  fetch(row);
+  if (group == 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * TPR + lane) * 8;
+      f32x2 g[4] = {};
+      if (c < D) params8(a.gamma, a.params_f32, c, D, g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) gamma[(i * 4 + e) * TPR + lane] = g[e];
+    }
+  }
+  __syncthreads();
+  f32x2 dg[NV][4] = {}, db[NV][4] = {};
+  const f32x2 minus_one = pair_of(-1.0f);
+  int parity = 0;
+  for (; row < a.T; row += (int64_t)gridDim.x * GROUPS, parity ^= 1) {
+    f32x2 h[NV][4], xh[NV][4], s1 = pair_of(0.0f), s2 = s1;  // (past D dy and gamma are 0)
+    const float2 st = st_next;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      values8(dy_next[i], h[i]);
+      values8(x_next[i], xh[i]);
+    }
+    fetch(row + (int64_t)gridDim.x * GROUPS);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if ((i * TPR + lane) * 8 >= D) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        xh[i][e] = mul2(fma2(minus_one, pair_of(st.x), xh[i][e]), pair_of(st.y));
+        dg[i][e] = fma2(h[i][e], xh[i][e], dg[i][e]);
+        db[i][e] = add2(h[i][e], db[i][e]);
+        h[i][e] = mul2(h[i][e], gamma[(i * 4 + e) * TPR + lane]);
+        s1 = add2(s1, h[i][e]);
+        s2 = fma2(h[i][e], xh[i][e], s2);
+      }
+    }
+    const float2 s = group_sum2<TPR>(sum_of(s1), sum_of(s2), slots + parity * kSlots<TPR>, group, lane);
+    const f32x2 c1 = pair_of(-(s.x * inv_D)), c2 = pair_of(-(s.y * inv_D)), r = pair_of(st.y);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + lane) * 8;
       if (c >= D) continue;
-      float dy[8], x[8], g[8];
-      values8(dyr[i], dy);
-      values8(xr[i], x);
-      params8(a.gamma, a.params_f32, c, D, g);
+      f32x2 o[4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {  // (past D dy and gamma are 0)
-        const float xh = (x[e] - st.x) * st.y, h = dy[e] * g[e];
-        dg[i][e] = fmaf(dy[e], xh, dg[i][e]);
-        db[i][e] += dy[e];
-        s.x += h;
-        s.y = fmaf(h, xh, s.y);
-      }
-    }
-    s = group_sum2<TPR>(s, slots[parity][group], group, lane);
-    const float c1 = s.x * inv_D, c2 = s.y * inv_D;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + lane) * 8;
-      if (c >= D) continue;
-      float dy[8], x[8], g[8], o[8];
-      values8(dyr[i], dy);
-      values8(xr[i], x);
-      params8(a.gamma, a.params_f32, c, D, g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float xh = (x[e] - st.x) * st.y;
-        o[e] = st.y * (fmaf(-xh, c2, dy[e] * g[e]) - c1);
-      }
+      for (int e = 0; e < 4; ++e) o[e] = mul2(add2(fma2(xh[i][e], c2, h[i][e]), c1), r);
       if (a.dx_f32)
         store_f32x8(static_cast<float*>(a.dx) + row * a.lddx, c, D, o);
       else
@@ -204,22 +265,23 @@ __global__ void __launch_bounds__(kThreadsOf<TPR>) norm_bwd_kernel(NormBwdArgs a
     }
   }
   // the groups' sums: the upper half of them adds to the lower one until one is left
+  __syncthreads();  // (gamma is done with)
 #pragma unroll
   for (int half = GROUPS / 2; half > 0; half >>= 1) {
-    float* mine = sums + (size_t)(group - (group >= half ? half : 0)) * (2 * NV * 8 * TPR) + lane;
+    f32x2* mine = sums + (size_t)(group - (group >= half ? half : 0)) * (2 * NV * 4 * TPR) + lane;
     if (group >= half && group < 2 * half) {
 #pragma unroll
-      for (int i = 0; i < NV * 8; ++i) {
-        mine[i * TPR] = dg[i >> 3][i & 7];
-        mine[(NV * 8 + i) * TPR] = db[i >> 3][i & 7];
+      for (int i = 0; i < NV * 4; ++i) {
+        mine[i * TPR] = dg[i >> 2][i & 3];
+        mine[(NV * 4 + i) * TPR] = db[i >> 2][i & 3];
       }
     }
     __syncthreads();
     if (group < half) {
 #pragma unroll
-      for (int i = 0; i < NV * 8; ++i) {
-        dg[i >> 3][i & 7] += mine[i * TPR];
-        db[i >> 3][i & 7] += mine[(NV * 8 + i) * TPR];
+      for (int i = 0; i < NV * 4; ++i) {
+        dg[i >> 2][i & 3] = add2(dg[i >> 2][i & 3], mine[i * TPR]);
+        db[i >> 2][i & 3] = add2(db[i >> 2][i & 3], mine[(NV * 4 + i) * TPR]);
       }
     }
     __syncthreads();
@@ -261,45 +323,46 @@ __global__ void __launch_bounds__(1024) norm_bwd_finish_kernel(const float* __re
     static_cast<uint16_t*>(out)[c] = (uint16_t)bf16x2_of(t, 0.0f);
 }
 
-// The shape of a row's group: as few threads as hold the row in at most four vectors each.
-template <typename F>
-cudaError_t with_shape(int D, F&& f) {
+// The shape of a row's group: as few threads as hold the row in MOST vectors each (three in forward, two in backward, whose registers hold
+// the columns' sums too), more vectors in the largest rows.
+template <int MOST, typename F>
+auto with_shape(int D, F&& f) {
+  using std::integral_constant;
   const int n8 = (D + 7) / 8;
-  auto nv = [&](auto tpr) {
-    constexpr int TPR = decltype(tpr)::value;
-    const int n = (n8 + TPR - 1) / TPR;
-    if constexpr (TPR == 32) {
-      if (n <= 1) return f(std::integral_constant<int, 1>{}, tpr);
-      if (n <= 2) return f(std::integral_constant<int, 2>{}, tpr);
-    }
-    if (n <= 3) return f(std::integral_constant<int, 3>{}, tpr);
-    return f(std::integral_constant<int, 4>{}, tpr);
-  };
-  if (n8 <= 128) return nv(std::integral_constant<int, 32>{});
-  if (n8 <= 256) return nv(std::integral_constant<int, 64>{});
-  if (n8 <= 512) return nv(std::integral_constant<int, 128>{});
-  if (n8 <= 1024) return nv(std::integral_constant<int, 256>{});
-  return nv(std::integral_constant<int, 512>{});
+  if (n8 <= 32) return f(integral_constant<int, 1>{}, integral_constant<int, 32>{});
+  if (n8 <= 64) return f(integral_constant<int, 2>{}, integral_constant<int, 32>{});
+  if (MOST >= 3 && n8 <= 96) return f(integral_constant<int, MOST>{}, integral_constant<int, 32>{});
+  if (n8 <= 128) return f(integral_constant<int, 2>{}, integral_constant<int, 64>{});
+  if (MOST >= 3 && n8 <= 192) return f(integral_constant<int, MOST>{}, integral_constant<int, 64>{});
+  if (n8 <= 256) return f(integral_constant<int, 2>{}, integral_constant<int, 128>{});
+  if (MOST >= 3 && n8 <= 384) return f(integral_constant<int, MOST>{}, integral_constant<int, 128>{});
+  if (n8 <= 512) return f(integral_constant<int, 2>{}, integral_constant<int, 256>{});
+  if (MOST >= 3 && n8 <= 768) return f(integral_constant<int, MOST>{}, integral_constant<int, 256>{});
+  if (n8 <= 1024) return f(integral_constant<int, 2>{}, integral_constant<int, 512>{});
+  if (n8 <= 1536) return f(integral_constant<int, 3>{}, integral_constant<int, 512>{});
+  return f(integral_constant<int, 4>{}, integral_constant<int, 512>{});
 }
 
 template <int SRC, bool CK>
 cudaError_t launch_norm_fwd(const NormFwdArgs& a, cudaStream_t st) {
-  return with_shape(a.D, [&](auto nv, auto tpr) {
+  return with_shape<3>(a.D, [&](auto nv, auto tpr) {
     constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value, GROUPS = kThreadsOf<TPR> / TPR;
-    return launch_kernel(norm_fwd_kernel<SRC, CK, NV, TPR>, dim3((unsigned)((a.T + GROUPS - 1) / GROUPS)), dim3(kThreadsOf<TPR>), 0, st, a);
+    return launch_kernel(norm_fwd_kernel<SRC, CK, NV, TPR>, dim3((unsigned)std::min<int64_t>((a.T + GROUPS - 1) / GROUPS, kFwdCtas)), dim3(kThreadsOf<TPR>), 0, st, a);
   });
 }
 
 int bwd_ctas(int64_t T, int D) {
-  const int groups = D <= 1024 ? 8 : D <= 2048 ? 4 : D <= 4096 ? 2 : 1;
-  return (int)std::min<int64_t>((T + groups - 1) / groups, kBwdCtas);
+  return with_shape<2>(D, [&](auto, auto tpr) {
+    constexpr int GROUPS = kThreadsOf<decltype(tpr)::value> / decltype(tpr)::value;
+    return (int)std::min<int64_t>((T + GROUPS - 1) / GROUPS, kBwdCtas);
+  });
 }
 
 template <int SRC>
 cudaError_t launch_norm_bwd(const NormBwdArgs& a, int ctas, cudaStream_t st) {
-  return with_shape(a.D, [&](auto nv, auto tpr) {
+  return with_shape<2>(a.D, [&](auto nv, auto tpr) {
     constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value, GROUPS = kThreadsOf<TPR> / TPR;
-    constexpr size_t smem = (size_t)(GROUPS / 2) * 2 * NV * 8 * TPR * sizeof(float);
+    constexpr size_t smem = (2 * kSlots<TPR> + (size_t)GROUPS * NV * 4 * TPR) * sizeof(f32x2);  // slots; gamma, or the sums of half the groups
     auto kernel = norm_bwd_kernel<SRC, NV, TPR>;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return e;

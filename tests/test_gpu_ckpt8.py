@@ -66,6 +66,8 @@ def test_every_border_of_the_format(dtype):
 def test_not_finite(dtype):
     x = inputs(6, 96, 4, torch.bfloat16)
     x[0, 3], x[1, 40], x[2, 95], x[3, :32], x[4, 0], x[5, 64:] = np.inf, -np.inf, np.nan, np.nan, -0.0, 0.0
+    x[0, 32:64:2] = np.nan  # every other element
+    x[1, :32], x[1, 5] = np.nan, 3.0
     pack_and_compare(x, dtype)
 
 
