@@ -130,7 +130,7 @@ struct Raw8<kSrcF32> {
 template <>
 struct Raw8<kSrcCkpt8> {
   uint2 q;
-  float scale;
+  uint32_t byte;  // of the scale (as it was loaded: arithmetic on it would wait for the load)
 };
 
 __device__ __forceinline__ f32x2 bf16_pair(uint32_t w) { return pair_of(bf16_lo(w), bf16_hi(w)); }
@@ -149,7 +149,7 @@ __device__ __forceinline__ void values8(const Raw8<kSrcF32>& r, f32x2 (&v)[4]) {
 __device__ __forceinline__ void values8(const Raw8<kSrcCkpt8>& r, f32x2 (&v)[4]) {  // exact
   ckpt8_decode(r.q, v);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], pair_of(r.scale));
+  for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], pair_of(ckpt8_scale(r.byte)));
 }
 // The largest magnitude of the eight, NaN left out (NaN where there is nothing else).
 __device__ __forceinline__ float amax8(const Raw8<kSrcBf16>& r) {
@@ -197,7 +197,7 @@ __device__ __forceinline__ Raw8<SRC> load8(const ActSrc& s, int64_t row, int c, 
     load_f32x8(static_cast<const float*>(s.p) + row * s.ld, c, D, r.lo, r.hi);
   } else {  // (codes past D are 0)
     r.q = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(s.p) + row * s.ld + c);
-    r.scale = ckpt8_scale(s.scales[row * (s.ld >> 5) + (c >> 5)]);
+    r.byte = s.scales[row * (s.ld >> 5) + (c >> 5)];
   }
   return r;
 }
