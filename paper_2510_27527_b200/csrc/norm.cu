@@ -16,14 +16,17 @@ namespace nvfp4 {
 namespace {
 
 constexpr int kMaxD = 16384;  // TPR 512, four vectors of eight a thread
-// CTAs, at most. Tuning constants, not hardware queries: the workspace size derived from backward's must not depend on the device.
-constexpr int kBwdCtas = 296, kFwdCtas = 888;
+// Backward: threads of a CTA (one per SM, 128 registers each) and CTAs, at most. Tuning constants, not hardware queries: the workspace size
+// derived from them must not depend on the device.
+constexpr int kBwdThreads = 512, kBwdCtas = 148;
 
 template <int TPR>
-constexpr int kThreadsOf = TPR < 256 ? 256 : TPR;  // of a CTA
+constexpr int kFwdThreadsOf = TPR < 128 ? 128 : TPR;  // of a CTA
+// Forward's threads per SM, by the registers that the shape needs (64 to 1024 threads, 96 to 640).
+template <int NV, int TPR>
+constexpr int kFwdThreadsPerSm = TPR == 32 && NV > 2 ? 640 : 1024;
 
-template <int TPR>
-constexpr int kSlots = kThreadsOf<TPR> / 32;  // of group_sum2, one set
+constexpr int kSlots = kBwdThreads / 32;  // of group_sum2, one set
 
 // eight parameters from column c on, 0 past D
 __device__ __forceinline__ void params8(const void* p, int f32, int c, int D, f32x2 (&v)[4]) {
@@ -38,7 +41,7 @@ __device__ __forceinline__ void params8(const void* p, int f32, int c, int D, f3
 
 template <int TPR>
 __device__ __forceinline__ void group_barrier(int group) {
-  if constexpr (kThreadsOf<TPR> == TPR)
+  if constexpr (TPR == 512)  // (the whole CTA)
     __syncthreads();
   else
     asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(TPR) : "memory");
@@ -94,10 +97,12 @@ struct NormFwdArgs {
 };
 
 template <int SRC, bool CK, int NV, int TPR>
-__global__ void __launch_bounds__(kThreadsOf<TPR>) norm_fwd_kernel(NormFwdArgs a) {
+__global__ void __launch_bounds__(kFwdThreadsOf<TPR>, kFwdThreadsPerSm<NV, TPR> / kFwdThreadsOf<TPR>) norm_fwd_kernel(NormFwdArgs a) {
   pdl_prologue();
-  constexpr int GROUPS = kThreadsOf<TPR> / TPR;
+  constexpr int GROUPS = kFwdThreadsOf<TPR> / TPR;
   __shared__ float slots[2][GROUPS][TPR / 32];
+  extern __shared__ __align__(16) uint8_t smem[];
+  ulonglong2* const params = reinterpret_cast<ulonglong2*>(smem);  // [gamma, beta][NV][2][TPR], four values each
   const int group = threadIdx.x / TPR, lane = threadIdx.x % TPR, D = a.D, ldc = (D + 31) & ~31;
   const float inv_D = 1.0f / (float)D;
   const f32x2 minus_one = pair_of(-1.0f);
@@ -112,15 +117,15 @@ __global__ void __launch_bounds__(kThreadsOf<TPR>) norm_fwd_kernel(NormFwdArgs a
   };
   int64_t row = (int64_t)blockIdx.x * GROUPS + group;
   fetch(row);
-  f32x2 g[NV][4], b[NV][4];
+  for (int j = group; j < 2 * NV; j += GROUPS) {
+    const int c = ((j >> 1) * TPR + lane) * 8;
+    f32x2 p[4] = {};
+    if (c < D && (j & 1) == 0) params8(a.gamma, a.params_f32, c, D, p);
+    if (c < D && (j & 1) && a.beta) params8(a.beta, a.params_f32, c, D, p);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (i * TPR + lane) * 8;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) g[i][e] = b[i][e] = pair_of(0.0f);
-    if (c < D) params8(a.gamma, a.params_f32, c, D, g[i]);
-    if (c < D && a.beta) params8(a.beta, a.params_f32, c, D, b[i]);
+    for (int e = 0; e < 2; ++e) params[(((j & 1) * NV + (j >> 1)) * 2 + e) * TPR + lane] = make_ulonglong2(p[2 * e], p[2 * e + 1]);
   }
+  __syncthreads();
   for (; row < a.T; row += (int64_t)gridDim.x * GROUPS) {
     f32x2 v[NV][4];
     float amax[NV];
@@ -167,7 +172,11 @@ __global__ void __launch_bounds__(kThreadsOf<TPR>) norm_fwd_kernel(NormFwdArgs a
       if (c >= D) continue;
       f32x2 o[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = fma2(mul2(v[i][e], pair_of(rstd)), g[i][e], b[i][e]);
+      for (int e = 0; e < 2; ++e) {
+        const ulonglong2 g = params[(i * 2 + e) * TPR + lane], b = params[((NV + i) * 2 + e) * TPR + lane];
+        o[2 * e] = fma2(mul2(v[i][2 * e], pair_of(rstd)), g.x, b.x);
+        o[2 * e + 1] = fma2(mul2(v[i][2 * e + 1], pair_of(rstd)), g.y, b.y);
+      }
       store_bf16x8(a.y + row * a.ldy, c, D, o);
     }
   }
@@ -185,13 +194,13 @@ struct NormBwdArgs {
 };
 
 template <int SRC, int NV, int TPR>
-__global__ void __launch_bounds__(kThreadsOf<TPR>, TPR > 256 ? 1 : 2) norm_bwd_kernel(NormBwdArgs a) {
+__global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(NormBwdArgs a) {
   pdl_prologue();
-  constexpr int GROUPS = kThreadsOf<TPR> / TPR;
+  constexpr int GROUPS = kBwdThreads / TPR;
   extern __shared__ __align__(16) uint8_t smem[];
   const int group = threadIdx.x / TPR, lane = threadIdx.x % TPR, D = a.D;
   float2* const slots = reinterpret_cast<float2*>(smem) + group * (TPR / 32);  // and again kSlots further on
-  f32x2* const gamma = reinterpret_cast<f32x2*>(smem) + 2 * kSlots<TPR>;       // [NV][4][TPR]
+  f32x2* const gamma = reinterpret_cast<f32x2*>(smem) + 2 * kSlots;       // [NV][4][TPR]
   f32x2* const sums = gamma;                            // and at the end, GROUPS / 2 times [dgamma, dbeta][NV][4][TPR]
   const float inv_D = 1.0f / (float)D;
   Raw8<kSrcBf16> dy_next[NV];
@@ -233,7 +242,16 @@ __global__ void __launch_bounds__(kThreadsOf<TPR>, TPR > 256 ? 1 : 2) norm_bwd_k
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       values8(dy_next[i], h[i]);
-      values8(x_next[i], xh[i]);
+      if constexpr (SRC == kSrcCkpt8) {  // code * (scale r) - m r: one rounding of 2^-24 of m r and one of the result
+        ckpt8_decode(x_next[i].q, xh[i]);
+        const f32x2 k = pair_of(ckpt8_scale(x_next[i].byte) * st.y), c = pair_of(-(st.x * st.y));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) xh[i][e] = fma2(xh[i][e], k, c);
+      } else {
+        values8(x_next[i], xh[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) xh[i][e] = mul2(fma2(minus_one, pair_of(st.x), xh[i][e]), pair_of(st.y));
+      }
     }
     fetch(row + (int64_t)gridDim.x * GROUPS);
 #pragma unroll
@@ -241,7 +259,6 @@ __global__ void __launch_bounds__(kThreadsOf<TPR>, TPR > 256 ? 1 : 2) norm_bwd_k
       if ((i * TPR + lane) * 8 >= D) continue;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        xh[i][e] = mul2(fma2(minus_one, pair_of(st.x), xh[i][e]), pair_of(st.y));
         dg[i][e] = fma2(h[i][e], xh[i][e], dg[i][e]);
         db[i][e] = add2(h[i][e], db[i][e]);
         h[i][e] = mul2(h[i][e], gamma[(i * 4 + e) * TPR + lane]);
@@ -249,7 +266,7 @@ __global__ void __launch_bounds__(kThreadsOf<TPR>, TPR > 256 ? 1 : 2) norm_bwd_k
         s2 = fma2(h[i][e], xh[i][e], s2);
       }
     }
-    const float2 s = group_sum2<TPR>(sum_of(s1), sum_of(s2), slots + parity * kSlots<TPR>, group, lane);
+    const float2 s = group_sum2<TPR>(sum_of(s1), sum_of(s2), slots + parity * kSlots, group, lane);
     const f32x2 c1 = pair_of(-(s.x * inv_D)), c2 = pair_of(-(s.y * inv_D)), r = pair_of(st.y);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -305,11 +322,12 @@ __global__ void __launch_bounds__(1024) norm_bwd_finish_kernel(const float* __re
   pdl_prologue();
   __shared__ float red[32][32];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, Dp = (D + 7) & ~7;
-  float s = 0.0f;
-  if (c < D) {
-#pragma unroll 4
-    for (int k = wid; k < rows; k += 32) s += partial[((size_t)k * 2 + blockIdx.y) * Dp + c];
-  }
+  constexpr int PER = (kBwdCtas + 31) / 32;  // rows of a warp, at most: all loads at once
+  float v[PER], s = 0.0f;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) v[k] = c < D && wid + 32 * k < rows ? partial[((size_t)(wid + 32 * k) * 2 + blockIdx.y) * Dp + c] : 0.0f;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) s += v[k];
   red[wid][lane] = s;
   __syncthreads();
   if (wid != 0 || c >= D) return;
@@ -343,17 +361,32 @@ auto with_shape(int D, F&& f) {
   return f(integral_constant<int, 4>{}, integral_constant<int, 512>{});
 }
 
+// Forward's: a warp holds up to 1024 elements, so that most rows need no barrier.
+template <typename F>
+auto with_fwd_shape(int D, F&& f) {
+  using std::integral_constant;
+  const int n8 = (D + 7) / 8;
+  if (n8 > 64 && n8 <= 96) return f(integral_constant<int, 3>{}, integral_constant<int, 32>{});
+  if (n8 > 64 && n8 <= 128) return f(integral_constant<int, 4>{}, integral_constant<int, 32>{});
+  return with_shape<3>(D, f);
+}
+
 template <int SRC, bool CK>
 cudaError_t launch_norm_fwd(const NormFwdArgs& a, cudaStream_t st) {
-  return with_shape<3>(a.D, [&](auto nv, auto tpr) {
-    constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value, GROUPS = kThreadsOf<TPR> / TPR;
-    return launch_kernel(norm_fwd_kernel<SRC, CK, NV, TPR>, dim3((unsigned)std::min<int64_t>((a.T + GROUPS - 1) / GROUPS, kFwdCtas)), dim3(kThreadsOf<TPR>), 0, st, a);
+  return with_fwd_shape(a.D, [&](auto nv, auto tpr) {
+    constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value, THREADS = kFwdThreadsOf<TPR>, GROUPS = THREADS / TPR;
+    constexpr size_t smem = (size_t)2 * NV * 2 * TPR * sizeof(ulonglong2);
+    auto kernel = norm_fwd_kernel<SRC, CK, NV, TPR>;
+    const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem + 1024);
+    if (e != cudaSuccess) return e;
+    const int64_t ctas = std::min<int64_t>((a.T + GROUPS - 1) / GROUPS, (int64_t)device_sm_count() * (kFwdThreadsPerSm<NV, TPR> / THREADS));
+    return launch_kernel(kernel, dim3((unsigned)ctas), dim3(THREADS), smem, st, a);
   });
 }
 
 int bwd_ctas(int64_t T, int D) {
   return with_shape<2>(D, [&](auto, auto tpr) {
-    constexpr int GROUPS = kThreadsOf<decltype(tpr)::value> / decltype(tpr)::value;
+    constexpr int GROUPS = kBwdThreads / decltype(tpr)::value;
     return (int)std::min<int64_t>((T + GROUPS - 1) / GROUPS, kBwdCtas);
   });
 }
@@ -361,12 +394,12 @@ int bwd_ctas(int64_t T, int D) {
 template <int SRC>
 cudaError_t launch_norm_bwd(const NormBwdArgs& a, int ctas, cudaStream_t st) {
   return with_shape<2>(a.D, [&](auto nv, auto tpr) {
-    constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value, GROUPS = kThreadsOf<TPR> / TPR;
-    constexpr size_t smem = (2 * kSlots<TPR> + (size_t)GROUPS * NV * 4 * TPR) * sizeof(f32x2);  // slots; gamma, or the sums of half the groups
+    constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value, GROUPS = kBwdThreads / TPR;
+    constexpr size_t smem = (2 * kSlots + (size_t)GROUPS * NV * 4 * TPR) * sizeof(f32x2);  // slots; gamma, or the sums of half the groups
     auto kernel = norm_bwd_kernel<SRC, NV, TPR>;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return e;
-    return launch_kernel(kernel, dim3((unsigned)ctas), dim3(kThreadsOf<TPR>), smem, st, a);
+    return launch_kernel(kernel, dim3((unsigned)ctas), dim3(kBwdThreads), smem, st, a);
   });
 }
 
