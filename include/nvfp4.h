@@ -446,7 +446,7 @@ nvfp4_status nvfp4_osci_sparse_suppress(float* W, int64_t ldw, int64_t C, int64_
  *   Y[m, n] = sum_k X[m, kept(k)] W-hat[n, k]  (+ sum_j X[m, outlier_cols[j]] W_out[n, j])  (+ bias[n]),  W-hat = P * S_block * S_global
  *
  *   X_bf16   [M, D], leading dimension ldx. Any M; every 32 tokens are one pass over the weights, meant for few tokens.
- *   W        operand [N, K] along the input channels in either scale layout and any gs_mode (nvfp4_quantize of the weights along AXIS_ROW,
+ *   W        operand [N, K] along the input channels, sf_layout TILED128x4, any gs_mode (nvfp4_quantize of the weights along AXIS_ROW,
  *            nvfp4_quantize_w16x16, or nvfp4_saved.qw of a forward call).
  *   n_out    0: K == D, and the three arguments after W are not looked at. Otherwise K + n_out == D; keep_cols [K] and outlier_cols [n_out]
  *            (device int32) say which column of X an operand column or an outlier stands for, W_out is BF16 [N, nvfp4_outlier_pad(n_out)],
@@ -454,13 +454,14 @@ nvfp4_status nvfp4_osci_sparse_suppress(float* W, int64_t ldw, int64_t C, int64_
  *            0 .. D-1 is read as NaN.
  *   bias     optional BF16 [N].
  *   Y        [M, N], leading dimension ldy, dtype y_dtype, 16-byte aligned rows. Columns from N on are left as they were.
+ *   dev_status optional, see nvfp4_gemm (the waits are for copies of the weights).
  * Products of X and P * S_block are exact, sums are FP32 in an order that M does not change; an element of X below 2^-28 of its token's
  * largest in 128 columns may lose up to 2^-39 of that largest one. Non-finite elements of X give non-finite results of their token.
  * Errors: NULL / ENUM / SHAPE (K + n_out != D, K <= 0) / LIMIT (M > 2097120, D > 2^30) / ALIGN / ARCH; nothing is launched on an error.
  * --------------------------------------------------------------------------------------------------------- */
 nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, const nvfp4_operand* W, const int32_t* keep_cols,
                         const int32_t* outlier_cols, int64_t n_out, const void* W_out, const void* bias_bf16, void* Y, int32_t y_dtype,
-                        int64_t ldy, void* stream);
+                        int64_t ldy, int32_t* dev_status, void* stream);
 
 /* ---------------------------------------------------------------------------------------------------------
  * Activation checkpoints in 8 bits: what the steps around the linears keep for backward, in half of BF16's bytes. (The linears themselves

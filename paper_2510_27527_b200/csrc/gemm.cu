@@ -1918,4 +1918,11 @@ cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t st) {
   return a.gs_mode == kGsTensor ? launch_tile128<kGsTensor>(a, st) : launch_tile128<kGsRow>(a, st);
 }
 
+bool encode_codes_map(void* tensor_map, const uint8_t* codes, int64_t R, int64_t Kp) {
+  return make_codes_map(static_cast<CUtensorMap*>(tensor_map), codes, R, Kp, 128);
+}
+bool encode_outliers_map(void* tensor_map, const void* base, int64_t R, int64_t Kh) {
+  return make_hp_map(static_cast<CUtensorMap*>(tensor_map), base, R, Kh, 128);
+}
+
 }  // namespace nvfp4

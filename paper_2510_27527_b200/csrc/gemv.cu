@@ -10,28 +10,33 @@
 // than 2^-39 of it. Every 128 k the FP32 result of the instructions is added to FP32 sums with the product of that power of two and the
 // weights' global scale, which is constant there in every scale mode.
 // The outlier channels go through BF16 instructions, 32 of them per step, with the same rows.
-// A CTA is four warps of 32 rows, a 128-row tile, because that is whose scale bytes lie together. A warp brings its rows' codes and scales
-// through a ring of its own in shared memory (asynchronous copies, kStages pieces ahead, no barrier between warps).
-// The k axis is split over the CTAs of a cluster, whose sums are added through distributed shared memory in a fixed order, one that M does
-// not change.
+// A CTA takes a 128-row tile, because that is whose scale bytes lie together, 256 k at a time: one tensor copy of 128 bytes of its rows (128-byte
+// swizzle), one of their scales, three or four of them in flight. Eight warps, 32 rows and one of the two halves of the 256 k each; the warp that is
+// the last to be done with a stage has it filled again. The k axis is split over the CTAs of a cluster as well. At the end every warp sends its
+// sums to the shared memory of the CTA that finishes these rows, which adds them up in a fixed order, one that M does not change.
+// Waits are for copies alone, and bounded.
 #include "../../include/nvfp4.h"
 
 #include "act8.cuh"
 #include "nvfp4_internal.h"
+#include "nvfp4_tc.cuh"
 
 namespace nvfp4 {
 
 namespace {
 
-constexpr int kRows = 128;       // weight rows of a CTA, 32 of a warp
-constexpr int kThreads = 128;
-constexpr int kStages = 4;       // pieces in flight per warp
-constexpr int kStageBytes = 2048 + 256 + 128;  // 32 rows of 64 bytes, their scales, their global scales
-constexpr int kSfAt = 2048, kGsAt = kSfAt + 256;
-constexpr int kRingBytes = 4 * kStages * kStageBytes;
-constexpr int kMaxTokens = 32;   // of one pass over the weights
+constexpr int kRows = 128;          // weight rows of a CTA, 32 of a warp
+constexpr int kThreads = 256;       // four row groups x two halves of k
+constexpr int kCodeBytes = 16384;   // of a stage: 128 rows x 128 bytes
+constexpr int kScaleBytes = 2048;   // four scale tiles
+constexpr int kStageBytes = kCodeBytes + kScaleBytes;
+constexpr int kMaxTokens = 32;      // of one pass over the weights
 constexpr int kMaxCluster = 8;
-constexpr int kXBytes = 64 * 1024;  // of staged X, at most
+// Stages, and bytes of staged X at most, by the tokens: two CTAs of up to 16 tokens share an SM, one of more has it to itself.
+template <int MT>
+constexpr int kStages = MT == 2 ? 3 : 4;
+template <int MT>
+constexpr int kXBytes = (MT == 1 ? 30 : MT == 2 ? 40 : 118) * 1024;
 
 struct GemvArgs {
   const uint16_t* X;
@@ -43,17 +48,17 @@ struct GemvArgs {
   const uint8_t *codes, *sf;
   const float* gscale;
   int64_t N;
-  int gs_mode, tiled;
+  int gs_mode;
   const uint16_t* bias;
   void* Y;
   int y_f32;
   int64_t ldy;
-  int n_codes, n_items;  // 128-k pieces of the codes; those and the 32-channel steps of the outliers
-  int seg;               // items staged at a time
+  int n_codes;           // 128-k pieces of the codes
+  int n_code_pairs, n_pairs;  // pairs of them; those and the pairs of 32-channel steps of the outliers
+  int seg;               // pairs whose X is staged at a time
+  int32_t* dev_status;
 };
 
-__device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
-__device__ __forceinline__ void copy4(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory"); }
 __device__ __forceinline__ uint4 shared16(uint32_t at) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
@@ -62,6 +67,11 @@ __device__ __forceinline__ uint4 shared16(uint32_t at) {
 __device__ __forceinline__ uint32_t shared_u16(uint32_t at) {
   uint16_t v;
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t shared_u32(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
   return v;
 }
 __device__ __forceinline__ float shared_f32(uint32_t at) {
@@ -79,8 +89,8 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// eight codes times the scale pair (both halves equal), as FP16 pairs in order
-__device__ __forceinline__ void weights8(uint32_t word, uint32_t scale2, uint32_t (&h)[4]) {
+// eight codes as FP16 pairs in order
+__device__ __forceinline__ void codes8(uint32_t word, uint32_t (&h)[4]) {
   asm("{\n"
       ".reg .b8 b0, b1, b2, b3;\n"
       "mov.b32 {b0, b1, b2, b3}, %4;\n"
@@ -91,12 +101,21 @@ __device__ __forceinline__ void weights8(uint32_t word, uint32_t scale2, uint32_
       "}"
       : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
       : "r"(word));
+}
+// and times the scale pair (both halves equal)
+__device__ __forceinline__ void weights8(uint32_t word, uint32_t scale2, uint32_t (&h)[4]) {
+  codes8(word, h);
   const __half2 s = *reinterpret_cast<const __half2*>(&scale2);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&h[i]), s);
     h[i] = *reinterpret_cast<const uint32_t*>(&p);
   }
+}
+__device__ __forceinline__ uint32_t scale_pair(uint32_t bytes) {  // the values of two E4M3 bytes as an FP16 pair
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)bytes));
+  return h;
 }
 // the values of two E4M3 bytes, each in both halves of a word
 __device__ __forceinline__ void scales2(uint32_t bytes, uint32_t (&s)[2]) {
@@ -105,12 +124,18 @@ __device__ __forceinline__ void scales2(uint32_t bytes, uint32_t (&s)[2]) {
   s[0] = __byte_perm(h, h, 0x1010);
   s[1] = __byte_perm(h, h, 0x3232);
 }
+// what the cluster's CTA `rank` holds at this address of its shared memory
 __device__ __forceinline__ float load_cluster(const float* p, uint32_t rank) {
   uint32_t at;
   float v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
   return v;
+}
+__device__ __forceinline__ uint32_t count_shared(uint32_t at) {  // the count before; releases what the thread read, acquires what the others did
+  uint32_t old;
+  asm volatile("atom.acq_rel.cta.shared::cta.add.u32 %0, [%1], 1;" : "=r"(old) : "r"(at) : "memory");
+  return old;
 }
 
 // Column `c` of the source that the operand's (or the outliers') column k stands for; -1 where it has none.
@@ -127,83 +152,99 @@ __device__ __forceinline__ uint4 x8(const uint16_t* row, const int32_t* cols, in
   return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
 }
 
-template <int MT, bool B128, bool TILED>  // MT: instructions' widths of eight tokens
-__global__ void __launch_bounds__(kThreads) gemv_kernel(GemvArgs a) {
-  pdl_prologue();
-  extern __shared__ __align__(16) uint8_t smem[];
-  constexpr int TOK = 8 * MT;
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+// MT: instructions' widths of eight tokens. SEP (up to two tokens): an instruction's eight columns are used for two tokens times four lanes, so
+// that each of its sums is over one lane's codes, which are of one block; the block scale then multiplies sums instead of codes.
+template <int MT, bool B128, bool SEP>
+__global__ void __launch_bounds__(kThreads, MT > 2 ? 1 : 2) gemv_kernel(const __grid_constant__ CUtensorMap codes_map, const __grid_constant__ CUtensorMap outliers_map, const GemvArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  constexpr int TOK = 8 * MT, STAGES = kStages<MT>;
+  __shared__ __align__(8) uint64_t full[STAGES];
+  __shared__ uint32_t done[STAGES];   // warps that are done with a stage, over all its uses
+  __shared__ uint32_t fills[STAGES];  // times that its copies were started
+  __shared__ int abort_flag;
+  const int warp = uniform_warp_index(), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int wrow = warp & 3, half = warp >> 2;
   uint32_t S, rank, rb;
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(S));
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm("mov.u32 %0, %%clusterid.x;" : "=r"(rb));
   const int64_t m0 = (int64_t)blockIdx.y * kMaxTokens;
   const int Mg = (int)min((int64_t)kMaxTokens, a.M - m0);
-  const int64_t row_w = (int64_t)rb * kRows + wid * 32;  // the warp's first row
-  const int64_t last = a.N - 1;                          // (rows past the end repeat the last one and are not stored)
-  const int64_t rs = min(row_w + lane, last);            // whose scales this lane brings
   const int Kp = (a.K + 127) & ~127;
-  const int64_t nb = Kp >> 4, nbp = (nb + 15) & ~(int64_t)15;
+  const int64_t nbp = ((Kp >> 4) + 15) & ~15;
 
-  uint8_t* xs = smem + kRingBytes;                                             // [piece][4][token][4] 16 bytes, then one piece of zeros
-  float* xscale = reinterpret_cast<float*>(xs + (size_t)(a.seg + 1) * 256 * Mg);  // [piece][TOK]
-  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + wid * (kStages * kStageBytes);
-  const uint32_t xs_at = (uint32_t)__cvta_generic_to_shared(xs), xscale_at = (uint32_t)__cvta_generic_to_shared(xscale);
+  const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;  // (swizzled copies)
+  uint8_t* xs = smem_raw + (ring - smem_u32(smem_raw)) + STAGES * kStageBytes;     // [piece][4][token][4] 16 bytes, then one piece of zeros
+  float* xscale = reinterpret_cast<float*>(xs + (size_t)(2 * a.seg + 1) * 256 * Mg);  // [piece][TOK]
+  float* red = xscale + 2 * a.seg * TOK;                                          // [half][token][row]
+  const uint32_t xs_at = smem_u32(xs), xscale_at = smem_u32(xscale);
+  const int p_begin = (int)(rank * (uint32_t)a.n_pairs / S), p_end = (int)((rank + 1) * (uint32_t)a.n_pairs / S);
 
-  const int i_begin = (int)(rank * (uint32_t)a.n_items / S), i_end = (int)((rank + 1) * (uint32_t)a.n_items / S);
-  const uint8_t *c[4], *o[4];
+  if (threadIdx.x == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&codes_map) : "memory");
+    abort_flag = 0;
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(smem_u32(&full[s]), 1);
+      done[s] = fills[s] = 0;
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  // pair p into its stage; one thread
+  auto fetch = [&](int p) {
+    const int s = (p - p_begin) % STAGES;
+    fills[s] += 1;
+    const uint32_t to = ring + s * kStageBytes, bar = smem_u32(&full[s]);
+    if (p < a.n_code_pairs) {
+      mbar_expect_tx(bar, kStageBytes, 1);
+      tma_load_2d(to, &codes_map, p * 128, (int32_t)(rb * kRows), bar, 1);
+      bulk_load(to + kCodeBytes, a.sf + ((int64_t)rb * (nbp >> 2) + (int64_t)p * 4) * 512, kScaleBytes, bar, 1);
+    } else {
+      mbar_expect_tx(bar, kCodeBytes, 1);
+      tma_load_2d(to, &outliers_map, (p - a.n_code_pairs) * 64, (int32_t)(rb * kRows), bar, 1);
+    }
+  };
+  pdl_wait();
+  if (threadIdx.x == 0)
+    for (int p = p_begin; p < min(p_end, p_begin + STAGES); ++p) fetch(p);
+  for (int i = threadIdx.x; i < 16 * Mg; i += kThreads) *reinterpret_cast<uint4*>(xs + (size_t)2 * a.seg * 256 * Mg + i * 16) = make_uint4(0, 0, 0, 0);
+
+  // the global scales of the four rows whose results this lane holds
+  const float* gs[4];
+  float gv[4] = {}, gv_next[4] = {};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const int64_t r = min(row_w + g + 8 * j, last);
-    c[j] = a.codes + r * (Kp >> 1) + t * 16;
-    o[j] = reinterpret_cast<const uint8_t*>(a.W_out) + r * a.Kh * 2 + t * 16;
+    const int64_t r = min((int64_t)rb * kRows + wrow * 32 + g + 8 * j, a.N - 1);
+    gs[j] = a.gscale + (B128 ? r * (Kp >> 7) : a.gs_mode == kGsRow ? r : 0);
+    if (!B128) gv[j] = *gs[j];
   }
-  const uint8_t* sf = a.sf + (TILED ? (int64_t)sf_tiled_offset(rs, 0, nbp) : rs * nb);
-  const float* gs = a.gscale + (B128 ? rs * (Kp >> 7) : 0);
-  float gv[4] = {};
-  if (!B128)
+  auto fetch_gs = [&](int i) {  // of piece i
+    if (B128 && i < a.n_codes)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) gv[j] = a.gscale[a.gs_mode == kGsRow ? min(row_w + g + 8 * j, last) : 0];
-
-  // piece i into its place in the ring; one group of copies, empty past the end
-  auto fetch = [&](int i) {
-    if (i < i_end) {
-      const uint32_t to = ring + (uint32_t)(i & (kStages - 1)) * kStageBytes;
-      if (i < a.n_codes) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) copy16(to + j * 512 + lane * 16, c[j] + (int64_t)i * 64);
-        copy4(to + kSfAt + lane * 8, sf + (int64_t)i * (TILED ? 1024 : 8));  // four blocks' scales, and the next four's
-        copy4(to + kSfAt + lane * 8 + 4, sf + (int64_t)i * (TILED ? 1024 : 8) + (TILED ? 512 : 4));
-        if (B128) copy4(to + kGsAt + lane * 4, gs + i);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) copy16(to + j * 512 + lane * 16, o[j] + (int64_t)(i - a.n_codes) * 64);
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+      for (int j = 0; j < 4; ++j) gv_next[j] = gs[j][i];
   };
-#pragma unroll
-  for (int p = 0; p < kStages; ++p) fetch(i_begin + p);
-  for (int i = threadIdx.x; i < 16 * Mg; i += kThreads) *reinterpret_cast<uint4*>(xs + (size_t)a.seg * 256 * Mg + i * 16) = make_uint4(0, 0, 0, 0);
+  fetch_gs(2 * p_begin + half);
 
   // where this lane's X lies in a piece, for each eight tokens; tokens that do not exist are read from the zeros
   uint32_t b_at[MT], b_step[MT];
 #pragma unroll
   for (int n = 0; n < MT; ++n) {
-    const bool live = n * 8 + g < Mg;
-    b_at[n] = xs_at + (live ? ((n * 8 + g) * 4 + t) * 16 : a.seg * 256 * Mg);
+    const int m = SEP ? g >> 2 : n * 8 + g;
+    const bool live = m < Mg && (!SEP || (g & 3) == t);
     b_step[n] = live ? 256 * Mg : 0;
+    b_at[n] = xs_at + (live ? (m * 4 + t) * 16 + half * 256 * Mg : 2 * a.seg * 256 * Mg);
   }
 
   float acc[2][MT][4] = {};
-  for (int s0 = i_begin; s0 < i_end; s0 += a.seg) {
-    const int n_seg = min(a.seg, i_end - s0);
-    if (s0 > i_begin) __syncthreads();
+  int s = 0;  // the stage
+  uint32_t phase = 0;
+  for (int q0 = p_begin; q0 < p_end; q0 += a.seg) {
+    const int s0 = 2 * q0, n_seg = 2 * min(a.seg, p_end - q0);  // pieces
+    if (q0 > p_begin) __syncthreads();
     // X: 16 lanes take a token's 128 values of a piece (or the 32 of an outlier step: 4 lanes of them), eight each; kAhead loads at a time
     {
       constexpr int kAhead = 4;
       const int l16 = lane & 15, n_units = n_seg * Mg;
-      for (int u0 = wid * 2 + (lane >> 4); u0 - (lane >> 4) < n_units; u0 += kAhead * (kThreads / 16)) {  // (a warp's two halves stay together)
+      for (int u0 = warp * 2 + (lane >> 4); u0 - (lane >> 4) < n_units; u0 += kAhead * (kThreads / 16)) {  // (a warp's two halves stay together)
         uint4 w[kAhead];
         int it[kAhead], m[kAhead];
 #pragma unroll
@@ -216,10 +257,10 @@ __global__ void __launch_bounds__(kThreads) gemv_kernel(GemvArgs a) {
             m[p] = u - it[p] * Mg;
             const int i = s0 + it[p];
             const uint16_t* row = a.X + (m0 + m[p]) * a.ldx;
-            if (i < a.n_codes)
+            if (i < 2 * a.n_code_pairs)
               w[p] = x8(row, a.keep, i * 128 + l16 * 8, a.K, a.D);
             else if (l16 < 4)
-              w[p] = x8(row, a.outl, (i - a.n_codes) * 32 + l16 * 8, a.n_out, a.D);
+              w[p] = x8(row, a.outl, (i - 2 * a.n_code_pairs) * 32 + l16 * 8, a.n_out, a.D);
           }
         }
 #pragma unroll
@@ -232,7 +273,7 @@ __global__ void __launch_bounds__(kThreads) gemv_kernel(GemvArgs a) {
           if (u >= n_units) continue;
           const uint32_t e = max(big >> 7, 15u);
           uint8_t* at = xs + (size_t)it[p] * 256 * Mg;
-          if (s0 + it[p] < a.n_codes) {
+          if (s0 + it[p] < 2 * a.n_code_pairs) {
             const float to = __uint_as_float((268u - e) << 23);  // 2^(141 - e)
             const uint32_t wj[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
             uint32_t h[4];
@@ -254,130 +295,186 @@ __global__ void __launch_bounds__(kThreads) gemv_kernel(GemvArgs a) {
     uint32_t b_now[MT];
 #pragma unroll
     for (int n = 0; n < MT; ++n) b_now[n] = b_at[n];
-    uint32_t xsc_now = xscale_at + 8 * t;
-    const int s_codes = min(s0 + n_seg, a.n_codes);
-    int i = s0;
+    uint32_t xsc_now = xscale_at + half * TOK * 4 + (SEP ? 4 * (t >> 1) : 8 * t);
 #pragma unroll 1
-    for (; i < s_codes; ++i) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-      __syncwarp();
-      const uint32_t at = ring + (uint32_t)(i & (kStages - 1)) * kStageBytes;
-      uint32_t wv[4][4], sc[4][2];
+    for (int p = q0; p < q0 + n_seg / 2; ++p) {
+      if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&full[s]), phase, &abort_flag, a.dev_status, DEFAULT_WAIT_LIMIT_CYCLES))) break;
+      const uint32_t at = ring + s * kStageBytes;
+      const int i = 2 * p + half;  // this warp's piece
+      uint32_t wv[4][4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint4 w = shared16(at + j * 512 + lane * 16);
+        const uint4 w = shared16(at + (wrow * 32 + 8 * j + g) * 128 + (((half * 4 + t) ^ g) << 4));
         wv[j][0] = w.x; wv[j][1] = w.y; wv[j][2] = w.z; wv[j][3] = w.w;
-        scales2(shared_u16(at + kSfAt + (g + 8 * j) * 8 + t * 2), sc[j]);
-        if (B128) gv[j] = shared_f32(at + kGsAt + (g + 8 * j) * 4);
+      }
+      const bool code = p < a.n_code_pairs;
+      uint32_t sc[4][2];
+      if (code) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (SEP) {  // of two lanes' two blocks each
+            const uint32_t four = shared_u32(at + kCodeBytes + (half * 2 + (t & 1)) * 512 + (8 * j + g) * 16 + wrow * 4);
+            sc[j][0] = scale_pair(four & 0xFFFFu);
+            sc[j][1] = scale_pair(four >> 16);
+          } else scales2(shared_u16(at + kCodeBytes + (half * 2 + (t >> 1)) * 512 + (8 * j + g) * 16 + wrow * 4 + (t & 1) * 2), sc[j]);
+          if (B128) gv[j] = gv_next[j];
+        }
+        fetch_gs(i + 2);
       }
       __syncwarp();
-      fetch(i + kStages);
-      float d[2][MT][4] = {};
+      if (lane == 0 && (count_shared(smem_u32(&done[s])) & 7u) == 7u && p + STAGES < p_end) fetch(p + STAGES);
+      if (SEP && code && i < a.n_codes) {
+        const float x0 = shared_f32(xsc_now);
 #pragma unroll
-      for (int wd = 0; wd < 4; ++wd) {
-        uint32_t h[4][4];
+        for (int k = 0; k < 2; ++k) {  // rows g and g + 8, then g + 16 and g + 24
+          float sum[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) weights8(wv[j][wd], sc[j][wd >> 1], h[j]);
+          for (int b = 0; b < 2; ++b) {  // the lanes' first block, then their second
+            float d[4] = {};
+#pragma unroll
+            for (int wd = 2 * b; wd < 2 * b + 2; ++wd) {
+              uint32_t h0[4], h1[4];
+              codes8(wv[2 * k][wd], h0);
+              codes8(wv[2 * k + 1][wd], h1);
+              const uint4 x = shared16(b_now[0] + (uint32_t)(wd * Mg) * 64);
+              mma_f16(d, h0[0], h1[0], h0[1], h1[1], x.x, x.y);
+              mma_f16(d, h0[2], h1[2], h0[3], h1[3], x.z, x.w);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {  // column 2 t + (e & 1): lane (2 t + (e & 1)) & 3 of token t >> 1
+              const float2 scale = __half22float2(*reinterpret_cast<const __half2*>(&sc[2 * k + (e >> 1)][e & 1]));
+              sum[e] = b == 0 ? d[e] * scale.x : fmaf(d[e], scale.y, sum[e]);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[k][0][e] = fmaf(sum[e], x0 * gv[2 * k + (e >> 1)], acc[k][0][e]);
+        }
+      } else if (!SEP && code && i < a.n_codes) {
+        float d[2][MT][4] = {};
+#pragma unroll
+        for (int wd = 0; wd < 4; ++wd) {
+          uint32_t h[4][4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) weights8(wv[j][wd], sc[j][wd >> 1], h[j]);
+#pragma unroll
+          for (int n = 0; n < MT; ++n) {
+            const uint4 b = shared16(b_now[n] + (uint32_t)(wd * Mg) * 64);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              mma_f16(d[k][n], h[2 * k][0], h[2 * k + 1][0], h[2 * k][1], h[2 * k + 1][1], b.x, b.y);
+              mma_f16(d[k][n], h[2 * k][2], h[2 * k + 1][2], h[2 * k][3], h[2 * k + 1][3], b.z, b.w);
+            }
+          }
+        }
 #pragma unroll
         for (int n = 0; n < MT; ++n) {
-          const uint4 b = shared16(b_now[n] + (uint32_t)(wd * Mg) * 64);
+          const float x0 = shared_f32(xsc_now + n * 32), x1 = shared_f32(xsc_now + n * 32 + 4);
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            mma_f16(d[k][n], h[2 * k][0], h[2 * k + 1][0], h[2 * k][1], h[2 * k + 1][1], b.x, b.y);
-            mma_f16(d[k][n], h[2 * k][2], h[2 * k + 1][2], h[2 * k][3], h[2 * k + 1][3], b.z, b.w);
+            acc[k][n][0] = fmaf(d[k][n][0], x0 * gv[2 * k], acc[k][n][0]);
+            acc[k][n][1] = fmaf(d[k][n][1], x1 * gv[2 * k], acc[k][n][1]);
+            acc[k][n][2] = fmaf(d[k][n][2], x0 * gv[2 * k + 1], acc[k][n][2]);
+            acc[k][n][3] = fmaf(d[k][n][3], x1 * gv[2 * k + 1], acc[k][n][3]);
+          }
+        }
+      } else if (!code) {  // 32 outlier channels
+#pragma unroll
+        for (int n = 0; n < MT; ++n) {
+          const uint4 b = shared16(b_now[n]);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float d[4] = {};
+            mma_bf16(d, wv[2 * k][0], wv[2 * k + 1][0], wv[2 * k][1], wv[2 * k + 1][1], b.x, b.y);
+            mma_bf16(d, wv[2 * k][2], wv[2 * k + 1][2], wv[2 * k][3], wv[2 * k + 1][3], b.z, b.w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[k][n][e] += d[e];
           }
         }
       }
 #pragma unroll
-      for (int n = 0; n < MT; ++n) {
-        const float x0 = shared_f32(xsc_now + n * 32), x1 = shared_f32(xsc_now + n * 32 + 4);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          acc[k][n][0] = fmaf(d[k][n][0], x0 * gv[2 * k], acc[k][n][0]);
-          acc[k][n][1] = fmaf(d[k][n][1], x1 * gv[2 * k], acc[k][n][1]);
-          acc[k][n][2] = fmaf(d[k][n][2], x0 * gv[2 * k + 1], acc[k][n][2]);
-          acc[k][n][3] = fmaf(d[k][n][3], x1 * gv[2 * k + 1], acc[k][n][3]);
-        }
-        b_now[n] += b_step[n];
+      for (int n = 0; n < MT; ++n) b_now[n] += 2 * b_step[n];
+      xsc_now += 2 * TOK * 4;
+      if (++s == STAGES) {
+        s = 0;
+        phase ^= 1u;
       }
-      xsc_now += TOK * 4;
     }
-#pragma unroll 1
-    for (; i < s0 + n_seg; ++i) {  // outlier channels
-      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-      __syncwarp();
-      const uint32_t at = ring + (uint32_t)(i & (kStages - 1)) * kStageBytes;
-      uint4 w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = shared16(at + j * 512 + lane * 16);
-      __syncwarp();
-      fetch(i + kStages);
-#pragma unroll
-      for (int n = 0; n < MT; ++n) {
-        const uint4 b = shared16(b_now[n]);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          float d[4] = {};
-          mma_bf16(d, w[2 * k].x, w[2 * k + 1].x, w[2 * k].y, w[2 * k + 1].y, b.x, b.y);
-          mma_bf16(d, w[2 * k].z, w[2 * k + 1].z, w[2 * k].w, w[2 * k + 1].w, b.z, b.w);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[k][n][e] += d[e];
-        }
-        b_now[n] += b_step[n];
+  }
+  pdl_launch_next();
+  __syncthreads();
+  if (abort_flag && threadIdx.x == 0) {  // a wait ran out: the copies under way get the same time to land before the CTA may end
+    for (int i = 0; i < STAGES; ++i) {
+      const long long t0 = clock64();
+      while (fills[i] > 0 && !mbar_test(smem_u32(&full[i]), (fills[i] - 1u) & 1u) && clock64() - t0 < DEFAULT_WAIT_LIMIT_CYCLES) {
       }
     }
   }
 
-  // the cluster's sums, where the rings were
-  __syncthreads();
-  float* red = reinterpret_cast<float*>(smem);  // [TOK][kRows]
+  // each warp's sums, then the cluster's
+  if (SEP) {  // the four lanes' sums of a token: two of them here, two in the neighbour
 #pragma unroll
-  for (int n = 0; n < MT; ++n)
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) red[(n * 8 + 2 * t + (e & 1)) * kRows + wid * 32 + g + (e >> 1) * 8] = acc[e >> 2][n][e & 3];
-  __syncthreads();
+      for (int e = 0; e < 4; e += 2) {
+        float v = acc[k][0][e] + acc[k][0][e + 1];
+        v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+        if ((t & 1) == 0 && (t >> 1) < Mg) red[(half * Mg + (t >> 1)) * kRows + wrow * 32 + k * 16 + g + (e >> 1) * 8] = v;
+      }
+  } else {
+#pragma unroll
+    for (int n = 0; n < MT; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int m = n * 8 + 2 * t + (e & 1);
+        if (m < Mg) red[(half * Mg + m) * kRows + wrow * 32 + g + (e >> 1) * 8] = acc[e >> 2][n][e & 3];
+      }
+  }
   if (S > 1) {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  } else {
+    __syncthreads();
   }
-  for (int i = rank * kThreads + threadIdx.x; i < Mg * kRows; i += S * kThreads) {
-    const int m = i / kRows, r = i % kRows;
+  const int rows = kRows / (int)S;  // that this CTA finishes
+  for (int i = threadIdx.x; i < Mg * rows; i += kThreads) {
+    const int m = i / rows, r = (int)rank * rows + (i - m * rows);
     const float* p = red + m * kRows + r;
-    float s = 0.0f;
-    if (S == 1)
-      s = *p;
-    else
-      for (uint32_t k = 0; k < S; ++k) s += load_cluster(p, k);
+    float v[2 * kMaxCluster], sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 2 * kMaxCluster; ++k)
+      if (k < 2 * (int)S) v[k] = S > 1 ? load_cluster(p + (k & 1) * Mg * kRows, (uint32_t)(k >> 1)) : p[(k & 1) * Mg * kRows];
+#pragma unroll
+    for (int k = 0; k < 2 * kMaxCluster; ++k)
+      if (k < 2 * (int)S) sum += v[k];
     const int64_t n = (int64_t)rb * kRows + r;
     if (n < a.N) {
-      if (a.bias) s += bf16_bits_to_float(a.bias[n]);
+      if (a.bias) sum += bf16_bits_to_float(a.bias[n]);
       if (a.y_f32)
-        static_cast<float*>(a.Y)[(m0 + m) * a.ldy + n] = s;
+        static_cast<float*>(a.Y)[(m0 + m) * a.ldy + n] = sum;
       else
-        static_cast<uint16_t*>(a.Y)[(m0 + m) * a.ldy + n] = (uint16_t)bf16x2_of(s, 0.0f);
+        static_cast<uint16_t*>(a.Y)[(m0 + m) * a.ldy + n] = (uint16_t)bf16x2_of(sum, 0.0f);
     }
   }
   if (S > 1) {  // (the others may still read from here)
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
   }
 }
 
-template <int MT, bool B128, bool TILED>
-cudaError_t launch_gemv(GemvArgs a, int64_t row_ctas, int S, cudaStream_t st) {
+template <int MT, bool B128, bool SEP>
+cudaError_t launch_gemv(const CUtensorMap& codes, const CUtensorMap& outliers, GemvArgs a, int64_t row_ctas, int S, cudaStream_t st) {
   const int Mg = (int)std::min<int64_t>(a.M, kMaxTokens);
-  const int per_cta = (a.n_items + S - 1) / S;
-  a.seg = std::max(1, std::min(per_cta, kXBytes / (256 * Mg)));
-  const size_t smem = kRingBytes + (size_t)(a.seg + 1) * 256 * Mg + (size_t)a.seg * 8 * MT * 4;
-  auto kernel = gemv_kernel<MT, B128, TILED>;
+  const int per_cta = (a.n_pairs + S - 1) / S;
+  a.seg = std::max(1, std::min(per_cta, (kXBytes<MT> / (256 * Mg) - 1) / 2));
+  const size_t smem = 1024 + kStages<MT> * kStageBytes + (size_t)(2 * a.seg + 1) * 256 * Mg + (size_t)2 * a.seg * 8 * MT * 4 + (size_t)2 * Mg * kRows * 4;
+  auto kernel = gemv_kernel<MT, B128, SEP>;
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
   if (e != cudaSuccess) return e;
-  return launch_kernel_cluster_smem(kernel, dim3((unsigned)(row_ctas * S), (unsigned)((a.M + kMaxTokens - 1) / kMaxTokens)), (unsigned)S, dim3(kThreads), smem, st, a);
+  return launch_kernel_cluster_smem(kernel, dim3((unsigned)(row_ctas * S), (unsigned)((a.M + kMaxTokens - 1) / kMaxTokens)), (unsigned)S, dim3(kThreads), smem, st, codes, outliers, a);
 }
-template <int MT>
-cudaError_t launch_gemv(const GemvArgs& a, int64_t row_ctas, int S, cudaStream_t st) {
-  if (a.gs_mode == kGsBlock128) return a.tiled ? launch_gemv<MT, true, true>(a, row_ctas, S, st) : launch_gemv<MT, true, false>(a, row_ctas, S, st);
-  return a.tiled ? launch_gemv<MT, false, true>(a, row_ctas, S, st) : launch_gemv<MT, false, false>(a, row_ctas, S, st);
+template <int MT, bool SEP>
+cudaError_t launch_gemv(const CUtensorMap& codes, const CUtensorMap& outliers, const GemvArgs& a, int64_t row_ctas, int S, cudaStream_t st) {
+  return a.gs_mode == kGsBlock128 ? launch_gemv<MT, true, SEP>(codes, outliers, a, row_ctas, S, st) : launch_gemv<MT, false, SEP>(codes, outliers, a, row_ctas, S, st);
 }
 
 }  // namespace
@@ -389,9 +486,9 @@ using namespace nvfp4;
 extern "C" {
 
 nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, const nvfp4_operand* W, const int32_t* keep_cols, const int32_t* outlier_cols,
-                        int64_t n_out, const void* W_out, const void* bias_bf16, void* Y, int32_t y_dtype, int64_t ldy, void* stream) {
+                        int64_t n_out, const void* W_out, const void* bias_bf16, void* Y, int32_t y_dtype, int64_t ldy, int32_t* dev_status, void* stream) {
   if (!W) return NVFP4_ERR_NULL;
-  if (W->gs_mode < 0 || W->gs_mode > 2 || W->sf_layout < 0 || W->sf_layout > 1 || y_dtype < 0 || y_dtype > 1) return NVFP4_ERR_ENUM;
+  if (W->gs_mode < 0 || W->gs_mode > 2 || W->sf_layout != NVFP4_SF_TILED128x4 || y_dtype < 0 || y_dtype > 1) return NVFP4_ERR_ENUM;
   if (M < 0 || D <= 0 || n_out < 0 || W->R < 0 || W->K <= 0 || W->K + n_out != D) return NVFP4_ERR_SHAPE;
   if (D > ((int64_t)1 << 30) || W->R > ((int64_t)1 << 31) || M > 65535ll * kMaxTokens) return NVFP4_ERR_LIMIT;
   if (M == 0 || W->R == 0) return NVFP4_OK;
@@ -416,19 +513,25 @@ nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, c
   a.gscale = W->gscale;
   a.N = W->R;
   a.gs_mode = W->gs_mode;
-  a.tiled = W->sf_layout == NVFP4_SF_TILED128x4;
   a.bias = static_cast<const uint16_t*>(bias_bf16);
   a.Y = Y;
   a.y_f32 = y_dtype == NVFP4_DT_F32;
   a.ldy = ldy;
   a.n_codes = (int)(nvfp4_padded_k(W->K) / 128);
-  a.n_items = a.n_codes + (n_out > 0 ? a.Kh / 32 : 0);
-  // CTAs along k
-  const int64_t row_ctas = (W->R + kRows - 1) / kRows, sms = device_sm_count();
+  a.n_code_pairs = (a.n_codes + 1) / 2;
+  a.n_pairs = a.n_code_pairs + a.Kh / 64;
+  a.dev_status = dev_status;
+  CUtensorMap codes{}, outliers{};
+  if (!encode_codes_map(&codes, W->codes, W->R, nvfp4_padded_k(W->K)) || (n_out > 0 && !encode_outliers_map(&outliers, W_out, W->R, a.Kh))) return NVFP4_ERR_CUDA;
+  // CTAs along k: as many as leave every CTA a pair and give an SM two of them
+  const int64_t row_ctas = (W->R + kRows - 1) / kRows, most = (int64_t)device_sm_count() * 2;
   int S = 1;
-  while (S < kMaxCluster && row_ctas * S * 2 <= sms * 4 && a.n_items >= 2 * S) S *= 2;
+  while (S < kMaxCluster && row_ctas * S * 2 <= most && a.n_pairs >= 2 * S) S *= 2;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = M <= 8 ? launch_gemv<1>(a, row_ctas, S, st) : M <= 16 ? launch_gemv<2>(a, row_ctas, S, st) : launch_gemv<4>(a, row_ctas, S, st);
+  const cudaError_t e = M <= 2    ? launch_gemv<1, true>(codes, outliers, a, row_ctas, S, st)
+                        : M <= 8  ? launch_gemv<1, false>(codes, outliers, a, row_ctas, S, st)
+                        : M <= 16 ? launch_gemv<2, false>(codes, outliers, a, row_ctas, S, st)
+                                  : launch_gemv<4, false>(codes, outliers, a, row_ctas, S, st);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
 }
 

@@ -189,6 +189,10 @@ struct GemmArgs {
 size_t gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int64_t gemm_block128_max_k();  // largest K the BLOCK128 GEMM variant takes
 cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t st);
+// Tensor maps (CUtensorMap) of an operand's codes and of a compact outlier matrix: boxes of 128 bytes x 128 rows, 128-byte swizzle, zeros
+// outside. False where the driver refuses.
+bool encode_codes_map(void* tensor_map, const uint8_t* codes, int64_t R, int64_t Kp);
+bool encode_outliers_map(void* tensor_map, const void* base, int64_t R, int64_t Kh);
 // C = (*a_gscale * *b_gscale) A B^T, A [M, ld] and B [N, ld] BF16 row-major (ld a multiple of 64), FP32 accumulation
 cudaError_t launch_dense_gemm(const void* A, const void* B, int64_t M, int64_t N, int64_t ld, const float* a_gscale,
                               const float* b_gscale, void* C, int c_is_f32, int64_t ldc, int32_t* dev_status, cudaStream_t st);
