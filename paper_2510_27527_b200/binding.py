@@ -116,7 +116,8 @@ EXPORTS = {
                                        c_vp]),
     "nvfp4_expand_operand": (c_i32, [ctypes.POINTER(COperand), ctypes.POINTER(CDenseOperand), c_vp]),
     "nvfp4_dense_gemm": (c_i32, [ctypes.POINTER(CDenseOperand), ctypes.POINTER(CDenseOperand), c_vp, c_i32, c_i64, c_vp, c_vp]),
-    "nvfp4_gemv": (c_i32, [c_vp, c_i64, c_i64, c_i64, ctypes.POINTER(COperand), c_vp, c_vp, c_i64, c_vp, c_vp, c_vp, c_i32, c_i64, c_vp, c_vp]),
+    "nvfp4_gemv_workspace_bytes": (c_sz, [c_i64, c_i64, c_i64]),
+    "nvfp4_gemv": (c_i32, [c_vp, c_i64, c_i64, c_i64, ctypes.POINTER(COperand), c_vp, c_vp, c_i64, c_vp, c_vp, c_vp, c_i32, c_i64, c_vp, c_vp, c_sz, c_vp]),
     "nvfp4_ckpt8_ld": (c_i64, [c_i64]),
     "nvfp4_ckpt8_pack": (c_i32, [c_vp, c_i32, c_i64, c_i64, c_i64, ctypes.POINTER(CCkpt8), c_vp]),
     "nvfp4_ckpt8_unpack": (c_i32, [ctypes.POINTER(CCkpt8), c_vp, c_i32, c_i64, c_vp]),

@@ -11,8 +11,8 @@
 // weights' global scale, which is constant there in every scale mode.
 // The outlier channels go through BF16 instructions, 32 of them per step, with the same rows.
 // A CTA takes a 128-row tile, because that is whose scale bytes lie together, 256 k at a time: one tensor copy of 128 bytes of its rows (128-byte
-// swizzle), one of their scales, three or four of them in flight. Eight warps, 32 rows and one of the two halves of the 256 k each; the warp that is
-// the last to be done with a stage has it filled again. The k axis is split over the CTAs of a cluster as well. At the end every warp sends its
+// swizzle), one of their scales, three or four of them in flight. One warp has them brought; eight take 32 rows and one of the
+// two halves of the 256 k each. The k axis is split over the CTAs of a cluster as well. At the end every warp sends its
 // sums to the shared memory of the CTA that finishes these rows, which adds them up in a fixed order, one that M does not change.
 // Waits are for copies alone, and bounded.
 #include "../../include/nvfp4.h"
@@ -26,17 +26,19 @@ namespace nvfp4 {
 namespace {
 
 constexpr int kRows = 128;          // weight rows of a CTA, 32 of a warp
-constexpr int kThreads = 256;       // four row groups x two halves of k
+constexpr int kConsumers = 256;     // four row groups x two halves of k
+constexpr int kThreads = kConsumers + 32;
 constexpr int kCodeBytes = 16384;   // of a stage: 128 rows x 128 bytes
 constexpr int kScaleBytes = 2048;   // four scale tiles
 constexpr int kStageBytes = kCodeBytes + kScaleBytes;
 constexpr int kMaxTokens = 32;      // of one pass over the weights
 constexpr int kMaxCluster = 8;
-// Stages, and bytes of staged X at most, by the tokens: two CTAs of up to 16 tokens share an SM, one of more has it to itself.
+// Two CTAs of up to 16 tokens share an SM, one of more has it to itself.
 template <int MT>
 constexpr int kStages = MT == 2 ? 3 : 4;
-template <int MT>
-constexpr int kXBytes = (MT == 1 ? 30 : MT == 2 ? 40 : 118) * 1024;
+constexpr int kXBytes = 30 * 1024;  // of X staged by the CTA itself, at most
+// A pair of pieces of X staged in memory: the values of both, then their powers of two.
+__host__ __device__ constexpr int pair_bytes(int tokens, int wide) { return 512 * tokens + 8 * wide; }
 
 struct GemvArgs {
   const uint16_t* X;
@@ -55,7 +57,9 @@ struct GemvArgs {
   int64_t ldy;
   int n_codes;           // 128-k pieces of the codes
   int n_code_pairs, n_pairs;  // pairs of them; those and the pairs of 32-channel steps of the outliers
-  int seg;               // pairs whose X is staged at a time
+  int seg;               // pairs whose X a CTA stages at a time
+  uint8_t* staged;       // X staged in memory: [32 tokens][pair] pair_bytes
+  int wide;              // tokens that an instruction's width is rounded to, of the kernel that reads it
   int32_t* dev_status;
 };
 
@@ -132,11 +136,7 @@ __device__ __forceinline__ float load_cluster(const float* p, uint32_t rank) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
   return v;
 }
-__device__ __forceinline__ uint32_t count_shared(uint32_t at) {  // the count before; releases what the thread read, acquires what the others did
-  uint32_t old;
-  asm volatile("atom.acq_rel.cta.shared::cta.add.u32 %0, [%1], 1;" : "=r"(old) : "r"(at) : "memory");
-  return old;
-}
+__device__ __forceinline__ void consumer_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(kConsumers) : "memory"); }
 
 // Column `c` of the source that the operand's (or the outliers') column k stands for; -1 where it has none.
 __device__ __forceinline__ uint32_t x_bits(const uint16_t* row, const int32_t* cols, int k, int n, int D) {
@@ -152,18 +152,67 @@ __device__ __forceinline__ uint4 x8(const uint16_t* row, const int32_t* cols, in
   return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
 }
 
+// One token's 128 values of a piece of X (or the 32 of an outlier step), by 16 lanes, eight each (4 of them).
+__device__ __forceinline__ uint4 load_piece(const GemvArgs& a, int64_t m, int i, int l16) {
+  const uint16_t* row = a.X + m * a.ldx;
+  if (i < 2 * a.n_code_pairs) return x8(row, a.keep, i * 128 + l16 * 8, a.K, a.D);
+  return l16 < 4 ? x8(row, a.outl, (i - 2 * a.n_code_pairs) * 32 + l16 * 8, a.n_out, a.D) : make_uint4(0, 0, 0, 0);
+}
+// Stores them as the instructions read them: [4 words of a lane's 16 codes][token][lane t] 16 bytes, and the power of two that they are to be
+// multiplied by again. Every lane of a warp calls this; `live`: this one's unit exists.
+__device__ __forceinline__ void store_piece(uint4 w, bool code, bool live, int l16, int m, int Mg, uint8_t* at, float* scale) {
+  const uint32_t m2 = amax16x2(amax16x2(w.x, w.y), amax16x2(w.z, w.w));
+  uint32_t big = max(m2 & 0x7FFFu, (m2 >> 16) & 0x7FFFu);  // (bit patterns of magnitudes are ordered like them)
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, o));
+  if (!live) return;
+  const uint32_t e = max(big >> 7, 15u);
+  if (code) {
+    const float to = __uint_as_float((268u - e) << 23);  // 2^(141 - e)
+    const uint32_t wj[4] = {w.x, w.y, w.z, w.w};
+    uint32_t h[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 v = values_of(mul2(bf16_pair(wj[j]), pair_of(to)));
+      const __half2 q = __floats2half2_rn(v.x, v.y);
+      h[j] = *reinterpret_cast<const uint32_t*>(&q);
+    }
+    *reinterpret_cast<uint4*>(at + (((l16 & 3) * Mg + m) * 4 + (l16 >> 2)) * 16) = make_uint4(h[0], h[1], h[2], h[3]);
+    if (l16 == 0) *scale = __uint_as_float((e - 14u) << 23);  // 2^(e - 141)
+  } else if (l16 < 4) {
+    *reinterpret_cast<uint4*>(at + (m * 4 + l16) * 16) = w;
+  }
+}
+
+// X staged in memory, for three and more tokens, whose staging in every CTA would take as long as the weights do (14336 x 4096 times 16 tokens:
+// 25.5 us then). It waits before it lets the product's CTAs start, so that those may read the weights at once.
+__global__ void __launch_bounds__(256) gemv_stage_kernel(const GemvArgs a) {
+  pdl_wait();
+  pdl_launch_next();
+  const int l16 = threadIdx.x & 15, pieces = 2 * a.n_pairs;
+  const int64_t u = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int64_t m = u <= 0xFFFFFFFFll ? (int64_t)((uint32_t)u / (uint32_t)pieces) : u / pieces;
+  const int i = (int)(u - m * pieces);
+  const bool live = m < a.M;
+  const int64_t group = m / kMaxTokens;
+  const int Mg = live ? (int)min((int64_t)kMaxTokens, a.M - group * kMaxTokens) : 1, mg = (int)(m - group * kMaxTokens);
+  uint8_t* at = a.staged + (group * a.n_pairs * pair_bytes(kMaxTokens, a.wide)) + (int64_t)(i >> 1) * pair_bytes(Mg, a.wide);
+  store_piece(live ? load_piece(a, m, i, l16) : make_uint4(0, 0, 0, 0), i < 2 * a.n_code_pairs, live, l16, mg, Mg, at + (i & 1) * 256 * Mg,
+              reinterpret_cast<float*>(at + 512 * Mg) + (i & 1) * a.wide + mg);
+}
+
 // MT: instructions' widths of eight tokens. SEP (up to two tokens): an instruction's eight columns are used for two tokens times four lanes, so
-// that each of its sums is over one lane's codes, which are of one block; the block scale then multiplies sums instead of codes.
+// that each of its sums is over one lane's codes, which are of one block; the block scale then multiplies sums instead of codes. X is staged by
+// the CTA; else it lies staged in memory and comes with the weights.
 template <int MT, bool B128, bool SEP>
 __global__ void __launch_bounds__(kThreads, MT > 2 ? 1 : 2) gemv_kernel(const __grid_constant__ CUtensorMap codes_map, const __grid_constant__ CUtensorMap outliers_map, const GemvArgs a) {
   extern __shared__ uint8_t smem_raw[];
   constexpr int TOK = 8 * MT, STAGES = kStages<MT>;
   __shared__ __align__(8) uint64_t full[STAGES];
-  __shared__ uint32_t done[STAGES];   // warps that are done with a stage, over all its uses
-  __shared__ uint32_t fills[STAGES];  // times that its copies were started
+  __shared__ __align__(8) uint64_t empty[STAGES];
   __shared__ int abort_flag;
   const int warp = uniform_warp_index(), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int wrow = warp & 3, half = warp >> 2;
+  const int wrow = warp & 3, half = (warp >> 2) & 1;
   uint32_t S, rank, rb;
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(S));
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -174,244 +223,241 @@ __global__ void __launch_bounds__(kThreads, MT > 2 ? 1 : 2) gemv_kernel(const __
   const int64_t nbp = ((Kp >> 4) + 15) & ~15;
 
   const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;  // (swizzled copies)
-  uint8_t* xs = smem_raw + (ring - smem_u32(smem_raw)) + STAGES * kStageBytes;     // [piece][4][token][4] 16 bytes, then one piece of zeros
-  float* xscale = reinterpret_cast<float*>(xs + (size_t)(2 * a.seg + 1) * 256 * Mg);  // [piece][TOK]
-  float* red = xscale + 2 * a.seg * TOK;                                          // [half][token][row]
-  const uint32_t xs_at = smem_u32(xs), xscale_at = smem_u32(xscale);
+  const int x_bytes = SEP ? 0 : pair_bytes(Mg, TOK), stage_bytes = kStageBytes + (x_bytes + 1023) / 1024 * 1024;
+  uint8_t* xs = smem_raw + (ring - smem_u32(smem_raw)) + STAGES * stage_bytes;     // SEP: [piece][4][token][4] 16 bytes; then one piece of zeros
+  float* xscale = reinterpret_cast<float*>(xs + (size_t)(SEP ? 2 * a.seg + 1 : 1) * 256 * Mg);  // SEP: [piece][TOK]
+  float* red = xscale + (SEP ? 2 * a.seg * TOK : 0);                              // [half][token][row]
+  const uint32_t xs_at = smem_u32(xs), xscale_at = smem_u32(xscale), zeros = xs_at + (SEP ? 2 * a.seg * 256 * Mg : 0);
   const int p_begin = (int)(rank * (uint32_t)a.n_pairs / S), p_end = (int)((rank + 1) * (uint32_t)a.n_pairs / S);
 
-  if (threadIdx.x == 0) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&codes_map) : "memory");
-    abort_flag = 0;
-    for (int s = 0; s < STAGES; ++s) {
-      mbar_init(smem_u32(&full[s]), 1);
-      done[s] = fills[s] = 0;
+  int filled = 0;  // stages that the bringing warp has had copied
+  if (warp == kConsumers / 32) {  // brings the weights
+    const uint32_t leader = elect_leader();
+    if (leader) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&codes_map) : "memory");
+      abort_flag = 0;
+      for (int i = 0; i < STAGES; ++i) {
+        mbar_init(smem_u32(&full[i]), 1);
+        mbar_init(smem_u32(&empty[i]), kConsumers / 32);
+      }
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  // pair p into its stage; one thread
-  auto fetch = [&](int p) {
-    const int s = (p - p_begin) % STAGES;
-    fills[s] += 1;
-    const uint32_t to = ring + s * kStageBytes, bar = smem_u32(&full[s]);
-    if (p < a.n_code_pairs) {
-      mbar_expect_tx(bar, kStageBytes, 1);
-      tma_load_2d(to, &codes_map, p * 128, (int32_t)(rb * kRows), bar, 1);
-      bulk_load(to + kCodeBytes, a.sf + ((int64_t)rb * (nbp >> 2) + (int64_t)p * 4) * 512, kScaleBytes, bar, 1);
-    } else {
-      mbar_expect_tx(bar, kCodeBytes, 1);
-      tma_load_2d(to, &outliers_map, (p - a.n_code_pairs) * 64, (int32_t)(rb * kRows), bar, 1);
+    __syncwarp();
+    asm volatile("bar.arrive 2, %0;" ::"n"(kThreads) : "memory");  // (the consumers wait there for the barriers)
+    int i = 0;
+    uint32_t phase = 1;
+    const uint8_t* const x = a.staged + (int64_t)blockIdx.y * a.n_pairs * pair_bytes(kMaxTokens, TOK);
+    auto bring_x = [&](int p, int i) {
+      bulk_load(ring + i * stage_bytes + kStageBytes, x + (int64_t)p * x_bytes, x_bytes, smem_u32(&full[i]), leader);
+    };
+    if (SEP) pdl_wait();
+    for (int p = p_begin; p < p_end; ++p) {
+      const uint32_t to = ring + i * stage_bytes, bar = smem_u32(&full[i]);
+      if (!SEP && p == p_begin + STAGES) {  // the first stages are full of weights: now X
+        pdl_wait();
+        for (int f = 0; f < STAGES; ++f) bring_x(p_begin + f, f);
+      }
+      if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&empty[i]), phase, &abort_flag, a.dev_status, DEFAULT_WAIT_LIMIT_CYCLES))) break;
+      if (p < a.n_code_pairs) {
+        mbar_expect_tx(bar, kStageBytes + x_bytes, leader);
+        tma_load_2d(to, &codes_map, p * 128, (int32_t)(rb * kRows), bar, leader);
+        bulk_load(to + kCodeBytes, a.sf + ((int64_t)rb * (nbp >> 2) + (int64_t)p * 4) * 512, kScaleBytes, bar, leader);
+      } else {
+        mbar_expect_tx(bar, kCodeBytes + x_bytes, leader);
+        tma_load_2d(to, &outliers_map, (p - a.n_code_pairs) * 64, (int32_t)(rb * kRows), bar, leader);
+      }
+      if (!SEP && p >= p_begin + STAGES) bring_x(p, i);
+      ++filled;
+      if (++i == STAGES) {
+        i = 0;
+        phase ^= 1u;
+      }
     }
-  };
-  pdl_wait();
-  if (threadIdx.x == 0)
-    for (int p = p_begin; p < min(p_end, p_begin + STAGES); ++p) fetch(p);
-  for (int i = threadIdx.x; i < 16 * Mg; i += kThreads) *reinterpret_cast<uint4*>(xs + (size_t)2 * a.seg * 256 * Mg + i * 16) = make_uint4(0, 0, 0, 0);
-
-  // the global scales of the four rows whose results this lane holds
-  const float* gs[4];
-  float gv[4] = {}, gv_next[4] = {};
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int64_t r = min((int64_t)rb * kRows + wrow * 32 + g + 8 * j, a.N - 1);
-    gs[j] = a.gscale + (B128 ? r * (Kp >> 7) : a.gs_mode == kGsRow ? r : 0);
-    if (!B128) gv[j] = *gs[j];
+    if (!SEP && p_end - p_begin <= STAGES) {
+      pdl_wait();
+      for (int f = 0; f < p_end - p_begin; ++f) bring_x(p_begin + f, f);
+    }
   }
-  auto fetch_gs = [&](int i) {  // of piece i
-    if (B128 && i < a.n_codes)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) gv_next[j] = gs[j][i];
-  };
-  fetch_gs(2 * p_begin + half);
-
-  // where this lane's X lies in a piece, for each eight tokens; tokens that do not exist are read from the zeros
-  uint32_t b_at[MT], b_step[MT];
-#pragma unroll
-  for (int n = 0; n < MT; ++n) {
-    const int m = SEP ? g >> 2 : n * 8 + g;
-    const bool live = m < Mg && (!SEP || (g & 3) == t);
-    b_step[n] = live ? 256 * Mg : 0;
-    b_at[n] = xs_at + (live ? (m * 4 + t) * 16 + half * 256 * Mg : 2 * a.seg * 256 * Mg);
-  }
-
   float acc[2][MT][4] = {};
-  int s = 0;  // the stage
-  uint32_t phase = 0;
-  for (int q0 = p_begin; q0 < p_end; q0 += a.seg) {
-    const int s0 = 2 * q0, n_seg = 2 * min(a.seg, p_end - q0);  // pieces
-    if (q0 > p_begin) __syncthreads();
-    // X: 16 lanes take a token's 128 values of a piece (or the 32 of an outlier step: 4 lanes of them), eight each; kAhead loads at a time
-    {
-      constexpr int kAhead = 4;
-      const int l16 = lane & 15, n_units = n_seg * Mg;
-      for (int u0 = warp * 2 + (lane >> 4); u0 - (lane >> 4) < n_units; u0 += kAhead * (kThreads / 16)) {  // (a warp's two halves stay together)
-        uint4 w[kAhead];
-        int it[kAhead], m[kAhead];
+  if (warp < kConsumers / 32) {
+    pdl_wait();
+    for (int i = threadIdx.x; i < 16 * Mg; i += kConsumers) *reinterpret_cast<uint4*>(xs + (zeros - xs_at) + i * 16) = make_uint4(0, 0, 0, 0);
+
+    // the global scales of the four rows whose results this lane holds
+    const float* gs[4];
+    float gv[4] = {}, gv_next[4] = {};
 #pragma unroll
-        for (int p = 0; p < kAhead; ++p) {
-          const int u = u0 + p * (kThreads / 16);
-          w[p] = make_uint4(0, 0, 0, 0);
-          it[p] = m[p] = 0;
-          if (u < n_units) {
-            it[p] = Mg == 1 ? u : u / Mg;
-            m[p] = u - it[p] * Mg;
-            const int i = s0 + it[p];
-            const uint16_t* row = a.X + (m0 + m[p]) * a.ldx;
-            if (i < 2 * a.n_code_pairs)
-              w[p] = x8(row, a.keep, i * 128 + l16 * 8, a.K, a.D);
-            else if (l16 < 4)
-              w[p] = x8(row, a.outl, (i - 2 * a.n_code_pairs) * 32 + l16 * 8, a.n_out, a.D);
-          }
-        }
-#pragma unroll
-        for (int p = 0; p < kAhead; ++p) {
-          const int u = u0 + p * (kThreads / 16);
-          const uint32_t m2 = amax16x2(amax16x2(w[p].x, w[p].y), amax16x2(w[p].z, w[p].w));
-          uint32_t big = max(m2 & 0x7FFFu, (m2 >> 16) & 0x7FFFu);  // (bit patterns of magnitudes are ordered like them)
-#pragma unroll
-          for (int o = 1; o < 16; o <<= 1) big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, o));
-          if (u >= n_units) continue;
-          const uint32_t e = max(big >> 7, 15u);
-          uint8_t* at = xs + (size_t)it[p] * 256 * Mg;
-          if (s0 + it[p] < 2 * a.n_code_pairs) {
-            const float to = __uint_as_float((268u - e) << 23);  // 2^(141 - e)
-            const uint32_t wj[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
-            uint32_t h[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float2 v = values_of(mul2(bf16_pair(wj[j]), pair_of(to)));
-              const __half2 q = __floats2half2_rn(v.x, v.y);
-              h[j] = *reinterpret_cast<const uint32_t*>(&q);
-            }
-            *reinterpret_cast<uint4*>(at + (((l16 & 3) * Mg + m[p]) * 4 + (l16 >> 2)) * 16) = make_uint4(h[0], h[1], h[2], h[3]);
-            if (l16 == 0) xscale[it[p] * TOK + m[p]] = __uint_as_float((e - 14u) << 23);  // 2^(e - 141)
-          } else if (l16 < 4) {
-            *reinterpret_cast<uint4*>(at + (m[p] * 4 + l16) * 16) = w[p];
-          }
-        }
-      }
+    for (int j = 0; j < 4; ++j) {
+      const int64_t r = min((int64_t)rb * kRows + wrow * 32 + g + 8 * j, a.N - 1);
+      gs[j] = a.gscale + (B128 ? r * (Kp >> 7) : a.gs_mode == kGsRow ? r : 0);
+      if (!B128) gv[j] = *gs[j];
     }
-    __syncthreads();
-    uint32_t b_now[MT];
+    auto fetch_gs = [&](int i) {  // of piece i
+      if (B128 && i < a.n_codes)
 #pragma unroll
-    for (int n = 0; n < MT; ++n) b_now[n] = b_at[n];
-    uint32_t xsc_now = xscale_at + half * TOK * 4 + (SEP ? 4 * (t >> 1) : 8 * t);
-#pragma unroll 1
-    for (int p = q0; p < q0 + n_seg / 2; ++p) {
-      if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&full[s]), phase, &abort_flag, a.dev_status, DEFAULT_WAIT_LIMIT_CYCLES))) break;
-      const uint32_t at = ring + s * kStageBytes;
-      const int i = 2 * p + half;  // this warp's piece
-      uint32_t wv[4][4];
+        for (int j = 0; j < 4; ++j) gv_next[j] = gs[j][i];
+    };
+    fetch_gs(2 * p_begin + half);
+
+    // where this lane's X lies in a staged pair, for each eight tokens; tokens that do not exist are read from the zeros
+    uint32_t b_at[MT];
+    bool live[MT];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint4 w = shared16(at + (wrow * 32 + 8 * j + g) * 128 + (((half * 4 + t) ^ g) << 4));
-        wv[j][0] = w.x; wv[j][1] = w.y; wv[j][2] = w.z; wv[j][3] = w.w;
+    for (int n = 0; n < MT; ++n) {
+      const int m = SEP ? g >> 2 : n * 8 + g;
+      live[n] = m < Mg && (!SEP || (g & 3) == t);
+      b_at[n] = (m * 4 + t) * 16 + half * 256 * Mg;
+    }
+
+    int s = 0;  // the stage
+    uint32_t phase = 0;
+    const int seg = SEP ? a.seg : p_end - p_begin;
+    for (int q0 = p_begin; q0 < p_end; q0 += seg) {
+      const int s0 = 2 * q0, n_seg = 2 * min(seg, p_end - q0);  // pieces
+      if (SEP) {
+        if (q0 > p_begin) consumer_barrier();
+        const int l16 = lane & 15, n_units = n_seg * Mg;
+        constexpr int kAhead = 4, kUnits = kConsumers / 16;  // loads at a time; units at a time
+        for (int u0 = warp * 2 + (lane >> 4); u0 - (lane >> 4) < n_units; u0 += kAhead * kUnits) {  // (a warp's two halves stay together)
+          uint4 w[kAhead];
+          int it[kAhead], m[kAhead];
+#pragma unroll
+          for (int p = 0; p < kAhead; ++p) {
+            const int u = u0 + p * kUnits;
+            it[p] = Mg == 1 ? u : u >> 1;  // (one token or two)
+            m[p] = Mg == 1 ? 0 : u & 1;
+            w[p] = u < n_units ? load_piece(a, m0 + m[p], s0 + it[p], l16) : make_uint4(0, 0, 0, 0);
+          }
+#pragma unroll
+          for (int p = 0; p < kAhead; ++p)
+            store_piece(w[p], s0 + it[p] < 2 * a.n_code_pairs, u0 + p * kUnits < n_units, l16, m[p], Mg, xs + (size_t)it[p] * 256 * Mg, xscale + it[p] * TOK + m[p]);
+        }
       }
-      const bool code = p < a.n_code_pairs;
-      uint32_t sc[4][2];
-      if (code) {
+      if (q0 == p_begin)
+        asm volatile("bar.sync 2, %0;" ::"n"(kThreads) : "memory");  // X is staged, the barriers are there
+      else
+        consumer_barrier();
+#pragma unroll 1
+      for (int p = q0; p < q0 + n_seg / 2; ++p) {
+        if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&full[s]), phase, &abort_flag, a.dev_status, DEFAULT_WAIT_LIMIT_CYCLES))) break;
+        const uint32_t at = ring + s * stage_bytes;
+        const int i = 2 * p + half;  // this warp's piece
+        const uint32_t xp = SEP ? xs_at + (p - q0) * 512 * Mg : at + kStageBytes;  // this pair of X
+        const uint32_t xsc = SEP ? xscale_at + (2 * (p - q0) + half) * TOK * 4 + 4 * (t >> 1) : xp + 512 * Mg + half * TOK * 4 + 8 * t;
+        uint32_t b_now[MT];
+#pragma unroll
+        for (int n = 0; n < MT; ++n) b_now[n] = live[n] ? xp + b_at[n] : zeros;
+        uint32_t wv[4][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          if (SEP) {  // of two lanes' two blocks each
-            const uint32_t four = shared_u32(at + kCodeBytes + (half * 2 + (t & 1)) * 512 + (8 * j + g) * 16 + wrow * 4);
-            sc[j][0] = scale_pair(four & 0xFFFFu);
-            sc[j][1] = scale_pair(four >> 16);
-          } else scales2(shared_u16(at + kCodeBytes + (half * 2 + (t >> 1)) * 512 + (8 * j + g) * 16 + wrow * 4 + (t & 1) * 2), sc[j]);
-          if (B128) gv[j] = gv_next[j];
+          const uint4 w = shared16(at + (wrow * 32 + 8 * j + g) * 128 + (((half * 4 + t) ^ g) << 4));
+          wv[j][0] = w.x; wv[j][1] = w.y; wv[j][2] = w.z; wv[j][3] = w.w;
         }
-        fetch_gs(i + 2);
-      }
-      __syncwarp();
-      if (lane == 0 && (count_shared(smem_u32(&done[s])) & 7u) == 7u && p + STAGES < p_end) fetch(p + STAGES);
-      if (SEP && code && i < a.n_codes) {
-        const float x0 = shared_f32(xsc_now);
+        const bool code = p < a.n_code_pairs;
+        uint32_t sc[4][2];
+        if (code) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {  // rows g and g + 8, then g + 16 and g + 24
-          float sum[4];
+          for (int j = 0; j < 4; ++j) {
+            if (SEP) {  // of two lanes' two blocks each
+              const uint32_t four = shared_u32(at + kCodeBytes + (half * 2 + (t & 1)) * 512 + (8 * j + g) * 16 + wrow * 4);
+              sc[j][0] = scale_pair(four & 0xFFFFu);
+              sc[j][1] = scale_pair(four >> 16);
+            } else scales2(shared_u16(at + kCodeBytes + (half * 2 + (t >> 1)) * 512 + (8 * j + g) * 16 + wrow * 4 + (t & 1) * 2), sc[j]);
+            if (B128) gv[j] = gv_next[j];
+          }
+          fetch_gs(i + 2);
+        }
+        if (SEP) {  // (else X is still to be read from the stage)
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&empty[s]));
+        }
+        if (SEP && code && i < a.n_codes) {
+          const float x0 = shared_f32(xsc);
+          float d[2][2][4] = {};  // [rows g, g + 8 / g + 16, g + 24][the lanes' first block / their second]: four chains of instructions
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {  // the lanes' first block, then their second
-            float d[4] = {};
+          for (int u = 0; u < 2; ++u) {
+            uint32_t h[4][2][4];
+            uint4 x[2];
 #pragma unroll
-            for (int wd = 2 * b; wd < 2 * b + 2; ++wd) {
-              uint32_t h0[4], h1[4];
-              codes8(wv[2 * k][wd], h0);
-              codes8(wv[2 * k + 1][wd], h1);
-              const uint4 x = shared16(b_now[0] + (uint32_t)(wd * Mg) * 64);
-              mma_f16(d, h0[0], h1[0], h0[1], h1[1], x.x, x.y);
-              mma_f16(d, h0[2], h1[2], h0[3], h1[3], x.z, x.w);
+            for (int b = 0; b < 2; ++b) {
+              x[b] = shared16(b_now[0] + (uint32_t)((2 * b + u) * Mg) * 64);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) codes8(wv[j][2 * b + u], h[j][b]);
             }
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) mma_f16(d[k][b], h[2 * k][b][0], h[2 * k + 1][b][0], h[2 * k][b][1], h[2 * k + 1][b][1], x[b].x, x[b].y);
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) mma_f16(d[k][b], h[2 * k][b][2], h[2 * k + 1][b][2], h[2 * k][b][3], h[2 * k + 1][b][3], x[b].z, x[b].w);
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {  // column 2 t + (e & 1): lane (2 t + (e & 1)) & 3 of token t >> 1
               const float2 scale = __half22float2(*reinterpret_cast<const __half2*>(&sc[2 * k + (e >> 1)][e & 1]));
-              sum[e] = b == 0 ? d[e] * scale.x : fmaf(d[e], scale.y, sum[e]);
+              acc[k][0][e] = fmaf(fmaf(d[k][1][e], scale.y, d[k][0][e] * scale.x), x0 * gv[2 * k + (e >> 1)], acc[k][0][e]);
+            }
+        } else if (!SEP && code && i < a.n_codes) {
+          float d[2][MT][4] = {};
+#pragma unroll
+          for (int wd = 0; wd < 4; ++wd) {
+            uint32_t h[4][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) weights8(wv[j][wd], sc[j][wd >> 1], h[j]);
+#pragma unroll
+            for (int n = 0; n < MT; ++n) {
+              const uint4 b = shared16(b_now[n] + (uint32_t)(wd * Mg) * 64);
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                mma_f16(d[k][n], h[2 * k][0], h[2 * k + 1][0], h[2 * k][1], h[2 * k + 1][1], b.x, b.y);
+                mma_f16(d[k][n], h[2 * k][2], h[2 * k + 1][2], h[2 * k][3], h[2 * k + 1][3], b.z, b.w);
+              }
             }
           }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[k][0][e] = fmaf(sum[e], x0 * gv[2 * k + (e >> 1)], acc[k][0][e]);
-        }
-      } else if (!SEP && code && i < a.n_codes) {
-        float d[2][MT][4] = {};
-#pragma unroll
-        for (int wd = 0; wd < 4; ++wd) {
-          uint32_t h[4][4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) weights8(wv[j][wd], sc[j][wd >> 1], h[j]);
 #pragma unroll
           for (int n = 0; n < MT; ++n) {
-            const uint4 b = shared16(b_now[n] + (uint32_t)(wd * Mg) * 64);
+            const float x0 = shared_f32(xsc + n * 32), x1 = shared_f32(xsc + n * 32 + 4);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              mma_f16(d[k][n], h[2 * k][0], h[2 * k + 1][0], h[2 * k][1], h[2 * k + 1][1], b.x, b.y);
-              mma_f16(d[k][n], h[2 * k][2], h[2 * k + 1][2], h[2 * k][3], h[2 * k + 1][3], b.z, b.w);
+              acc[k][n][0] = fmaf(d[k][n][0], x0 * gv[2 * k], acc[k][n][0]);
+              acc[k][n][1] = fmaf(d[k][n][1], x1 * gv[2 * k], acc[k][n][1]);
+              acc[k][n][2] = fmaf(d[k][n][2], x0 * gv[2 * k + 1], acc[k][n][2]);
+              acc[k][n][3] = fmaf(d[k][n][3], x1 * gv[2 * k + 1], acc[k][n][3]);
+            }
+          }
+        } else if (!code) {  // 32 outlier channels
+#pragma unroll
+          for (int n = 0; n < MT; ++n) {
+            const uint4 b = shared16(b_now[n]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              float d[4] = {};
+              mma_bf16(d, wv[2 * k][0], wv[2 * k + 1][0], wv[2 * k][1], wv[2 * k + 1][1], b.x, b.y);
+              mma_bf16(d, wv[2 * k][2], wv[2 * k + 1][2], wv[2 * k][3], wv[2 * k + 1][3], b.z, b.w);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[k][n][e] += d[e];
             }
           }
         }
-#pragma unroll
-        for (int n = 0; n < MT; ++n) {
-          const float x0 = shared_f32(xsc_now + n * 32), x1 = shared_f32(xsc_now + n * 32 + 4);
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            acc[k][n][0] = fmaf(d[k][n][0], x0 * gv[2 * k], acc[k][n][0]);
-            acc[k][n][1] = fmaf(d[k][n][1], x1 * gv[2 * k], acc[k][n][1]);
-            acc[k][n][2] = fmaf(d[k][n][2], x0 * gv[2 * k + 1], acc[k][n][2]);
-            acc[k][n][3] = fmaf(d[k][n][3], x1 * gv[2 * k + 1], acc[k][n][3]);
-          }
+        if (!SEP) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&empty[s]));
         }
-      } else if (!code) {  // 32 outlier channels
-#pragma unroll
-        for (int n = 0; n < MT; ++n) {
-          const uint4 b = shared16(b_now[n]);
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float d[4] = {};
-            mma_bf16(d, wv[2 * k][0], wv[2 * k + 1][0], wv[2 * k][1], wv[2 * k + 1][1], b.x, b.y);
-            mma_bf16(d, wv[2 * k][2], wv[2 * k + 1][2], wv[2 * k][3], wv[2 * k + 1][3], b.z, b.w);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[k][n][e] += d[e];
-          }
+        if (++s == STAGES) {
+          s = 0;
+          phase ^= 1u;
         }
-      }
-#pragma unroll
-      for (int n = 0; n < MT; ++n) b_now[n] += 2 * b_step[n];
-      xsc_now += 2 * TOK * 4;
-      if (++s == STAGES) {
-        s = 0;
-        phase ^= 1u;
       }
     }
   }
   pdl_launch_next();
-  __syncthreads();
-  if (abort_flag && threadIdx.x == 0) {  // a wait ran out: the copies under way get the same time to land before the CTA may end
-    for (int i = 0; i < STAGES; ++i) {
-      const long long t0 = clock64();
-      while (fills[i] > 0 && !mbar_test(smem_u32(&full[i]), (fills[i] - 1u) & 1u) && clock64() - t0 < DEFAULT_WAIT_LIMIT_CYCLES) {
-      }
-    }
-  }
 
   // each warp's sums, then the cluster's
-  if (SEP) {  // the four lanes' sums of a token: two of them here, two in the neighbour
+  if (warp >= kConsumers / 32) {
+  } else if (SEP) {  // the four lanes' sums of a token: two of them here, two in the neighbour
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -435,9 +481,8 @@ __global__ void __launch_bounds__(kThreads, MT > 2 ? 1 : 2) gemv_kernel(const __
   } else {
     __syncthreads();
   }
-  const int rows = kRows / (int)S;  // that this CTA finishes
-  for (int i = threadIdx.x; i < Mg * rows; i += kThreads) {
-    const int m = i / rows, r = (int)rank * rows + (i - m * rows);
+  for (int i = (int)rank * kThreads + threadIdx.x; i < Mg * kRows; i += (int)S * kThreads) {
+    const int m = i / kRows, r = i % kRows;
     const float* p = red + m * kRows + r;
     float v[2 * kMaxCluster], sum = 0.0f;
 #pragma unroll
@@ -455,6 +500,13 @@ __global__ void __launch_bounds__(kThreads, MT > 2 ? 1 : 2) gemv_kernel(const __
         static_cast<uint16_t*>(a.Y)[(m0 + m) * a.ldy + n] = (uint16_t)bf16x2_of(sum, 0.0f);
     }
   }
+  if (warp == kConsumers / 32 && *(volatile int*)&abort_flag) {  // a wait ran out: the copies under way get the same time to land before the CTA ends
+    for (int f = max(0, filled - STAGES); f < filled; ++f) {
+      const long long t0 = clock64();
+      while (!mbar_test(smem_u32(&full[f % STAGES]), (uint32_t)(f / STAGES) & 1u) && clock64() - t0 < DEFAULT_WAIT_LIMIT_CYCLES) {
+      }
+    }
+  }
   if (S > 1) {  // (the others may still read from here)
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
@@ -465,8 +517,15 @@ template <int MT, bool B128, bool SEP>
 cudaError_t launch_gemv(const CUtensorMap& codes, const CUtensorMap& outliers, GemvArgs a, int64_t row_ctas, int S, cudaStream_t st) {
   const int Mg = (int)std::min<int64_t>(a.M, kMaxTokens);
   const int per_cta = (a.n_pairs + S - 1) / S;
-  a.seg = std::max(1, std::min(per_cta, (kXBytes<MT> / (256 * Mg) - 1) / 2));
-  const size_t smem = 1024 + kStages<MT> * kStageBytes + (size_t)(2 * a.seg + 1) * 256 * Mg + (size_t)2 * a.seg * 8 * MT * 4 + (size_t)2 * Mg * kRows * 4;
+  a.seg = std::max(1, std::min(per_cta, (kXBytes / (256 * Mg) - 1) / 2));
+  a.wide = 8 * MT;
+  const size_t x = SEP ? (size_t)(2 * a.seg + 1) * 256 * Mg + (size_t)2 * a.seg * 8 * MT * 4 : (size_t)256 * Mg;
+  const size_t smem = 1024 + kStages<MT> * (kStageBytes + (SEP ? 0 : (pair_bytes(Mg, 8 * MT) + 1023) / 1024 * 1024)) + x + (size_t)2 * Mg * kRows * 4;
+  if (!SEP) {
+    const int64_t units = a.M * 2 * a.n_pairs;
+    const cudaError_t e = launch_kernel(gemv_stage_kernel, dim3((unsigned)((units + 15) / 16)), dim3(256), 0, st, a);
+    if (e != cudaSuccess) return e;
+  }
   auto kernel = gemv_kernel<MT, B128, SEP>;
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
   if (e != cudaSuccess) return e;
@@ -485,19 +544,30 @@ using namespace nvfp4;
 
 extern "C" {
 
+size_t nvfp4_gemv_workspace_bytes(int64_t M, int64_t D, int64_t n_out) {
+  if (M <= 2 || D <= 0 || n_out < 0 || n_out > D) return 0;
+  const int64_t pairs = (nvfp4_padded_k(D - n_out) / 128 + 1) / 2 + nvfp4_outlier_pad(n_out) / 64;
+  const int wide = M <= 8 ? 8 : M <= 16 ? 16 : 32;
+  return (size_t)(pairs * (M / kMaxTokens * pair_bytes(kMaxTokens, wide) + (M % kMaxTokens ? pair_bytes((int)(M % kMaxTokens), wide) : 0)));
+}
+
 nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, const nvfp4_operand* W, const int32_t* keep_cols, const int32_t* outlier_cols,
-                        int64_t n_out, const void* W_out, const void* bias_bf16, void* Y, int32_t y_dtype, int64_t ldy, int32_t* dev_status, void* stream) {
+                        int64_t n_out, const void* W_out, const void* bias_bf16, void* Y, int32_t y_dtype, int64_t ldy, int32_t* dev_status, void* workspace, size_t ws_bytes,
+                        void* stream) {
   if (!W) return NVFP4_ERR_NULL;
   if (W->gs_mode < 0 || W->gs_mode > 2 || W->sf_layout != NVFP4_SF_TILED128x4 || y_dtype < 0 || y_dtype > 1) return NVFP4_ERR_ENUM;
   if (M < 0 || D <= 0 || n_out < 0 || W->R < 0 || W->K <= 0 || W->K + n_out != D) return NVFP4_ERR_SHAPE;
-  if (D > ((int64_t)1 << 30) || W->R > ((int64_t)1 << 31) || M > 65535ll * kMaxTokens) return NVFP4_ERR_LIMIT;
+  if (D > ((int64_t)1 << 24) || W->R > ((int64_t)1 << 31) || M > 65535ll * kMaxTokens) return NVFP4_ERR_LIMIT;
   if (M == 0 || W->R == 0) return NVFP4_OK;
   if (!X_bf16 || !Y || !W->codes || !W->sf || !W->gscale || (n_out > 0 && (!keep_cols || !outlier_cols || !W_out))) return NVFP4_ERR_NULL;
   if (bad_matrix(X_bf16, ldx, D, 2) || bad_matrix(Y, ldy, W->R, y_dtype == NVFP4_DT_F32 ? 4 : 2) || !aligned(W->codes, 16) || !aligned(W->sf, 16) || !aligned(W->gscale, 4) ||
       !aligned(bias_bf16, 2) || (n_out > 0 && (!aligned(W_out, 16) || !aligned(keep_cols, 4) || !aligned(outlier_cols, 4))))
     return NVFP4_ERR_ALIGN;
+  if (M * ((D >> 7) + 4) > (int64_t)1 << 33) return NVFP4_ERR_LIMIT;  // (the grid that stages X)
+  if (M > 2 && (!workspace || !aligned(workspace, 16) || ws_bytes < nvfp4_gemv_workspace_bytes(M, D, n_out))) return NVFP4_ERR_WORKSPACE;
   if (!device_is_sm100()) return NVFP4_ERR_ARCH;
   GemvArgs a{};
+  a.staged = static_cast<uint8_t*>(workspace);
   a.X = static_cast<const uint16_t*>(X_bf16);
   a.ldx = ldx;
   a.M = M;
@@ -525,8 +595,7 @@ nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, c
   if (!encode_codes_map(&codes, W->codes, W->R, nvfp4_padded_k(W->K)) || (n_out > 0 && !encode_outliers_map(&outliers, W_out, W->R, a.Kh))) return NVFP4_ERR_CUDA;
   // CTAs along k: as many as leave every CTA a pair and give an SM two of them
   const int64_t row_ctas = (W->R + kRows - 1) / kRows, most = (int64_t)device_sm_count() * 2;
-  int S = 1;
-  while (S < kMaxCluster && row_ctas * S * 2 <= most && a.n_pairs >= 2 * S) S *= 2;
+  const int S = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(kMaxCluster, a.n_pairs), most / row_ctas));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = M <= 2    ? launch_gemv<1, true>(codes, outliers, a, row_ctas, S, st)
                         : M <= 8  ? launch_gemv<1, false>(codes, outliers, a, row_ctas, S, st)

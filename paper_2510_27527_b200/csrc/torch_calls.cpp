@@ -140,7 +140,10 @@ PyObject* gemv(PyObject*, Args a, Py_ssize_t n) {
   TORCH_CHECK(W.R >= 0, where, ": ", W.R, " weight rows");
   at::Tensor Y = given(a[13]) ? tensor(a[13], where, "out") : matrix(M, W.R, X.options().dtype(type));
   const int64_t ldy = rows_of(Y, where, "out", type, M, W.R, dev);
-  check(nvfp4_gemv(X.data_ptr(), ldx, M, D, &W, keep, outl, n_out, W_out, bias, Y.data_ptr(), code_of(type), ldy, nullptr, current_stream()), where);
+  const size_t need = nvfp4_gemv_workspace_bytes(M, D, n_out);
+  const at::Tensor ws = need ? at::empty({(int64_t)need}, X.options().dtype(at::kByte)) : at::Tensor();
+  check(nvfp4_gemv(X.data_ptr(), ldx, M, D, &W, keep, outl, n_out, W_out, bias, Y.data_ptr(), code_of(type), ldy, nullptr, need ? ws.data_ptr() : nullptr, need,
+                   current_stream()), where);
   return wrap(Y);
   END_HANDLE_TH_ERRORS
 }

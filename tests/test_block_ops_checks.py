@@ -12,21 +12,22 @@ OK, NULL, SHAPE, ALIGN, ENUM, WORKSPACE, LIMIT = 0, 1, 2, 3, 4, 5, 9
 
 
 def _gemv(**change):
-    a = dict(X=P, ldx=64, M=2, D=64, codes=Q, sf=R, gscale=S, N=40, K=64, gs=0, layout=1, keep=None, outl=None, n_out=0, wo=None, bias=None, Y=T, yt=0, ldy=40)
+    a = dict(X=P, ldx=64, M=2, D=64, codes=Q, sf=R, gscale=S, N=40, K=64, gs=0, layout=1, keep=None, outl=None, n_out=0, wo=None, bias=None, Y=T, yt=0, ldy=40, ws=None, n=0)
     a.update(change)
     w = b.COperand(a["codes"], a["sf"], a["gscale"], a["N"], a["K"], a["gs"], a["layout"])
-    return L.nvfp4_gemv(a["X"], a["ldx"], a["M"], a["D"], ctypes.byref(w), a["keep"], a["outl"], a["n_out"], a["wo"], a["bias"], a["Y"], a["yt"], a["ldy"], None, None)
+    return L.nvfp4_gemv(a["X"], a["ldx"], a["M"], a["D"], ctypes.byref(w), a["keep"], a["outl"], a["n_out"], a["wo"], a["bias"], a["Y"], a["yt"], a["ldy"], None, a["ws"], a["n"], None)
 
 
 @pytest.mark.parametrize("change,status", [
     (dict(M=0), OK), (dict(N=0), OK), (dict(X=None), NULL), (dict(Y=None), NULL), (dict(codes=None), NULL), (dict(sf=None), NULL), (dict(gscale=None), NULL),
     (dict(gs=3), ENUM), (dict(layout=2), ENUM), (dict(layout=0), ENUM), (dict(yt=2), ENUM), (dict(M=-1), SHAPE), (dict(D=0, K=0), SHAPE), (dict(K=32), SHAPE), (dict(N=-1), SHAPE),
-    (dict(K=60, n_out=4), NULL), (dict(K=60, n_out=4, keep=P, outl=P), NULL), (dict(K=60, n_out=4, keep=P, outl=P, wo=P + 8), ALIGN),
+    (dict(M=3), WORKSPACE), (dict(M=3, ws=P, n=511), WORKSPACE), (dict(M=3, ws=P + 8, n=1 << 20), WORKSPACE), (dict(K=60, n_out=4), NULL), (dict(K=60, n_out=4, keep=P, outl=P), NULL), (dict(K=60, n_out=4, keep=P, outl=P, wo=P + 8), ALIGN),
     (dict(n_out=-1, K=65), SHAPE), (dict(X=P + 8), ALIGN), (dict(ldx=60), ALIGN), (dict(ldx=56), ALIGN), (dict(Y=T + 4), ALIGN), (dict(ldy=36), ALIGN), (dict(ldy=44), ALIGN),
-    (dict(codes=Q + 8), ALIGN), (dict(gscale=S + 2), ALIGN), (dict(bias=P + 1), ALIGN), (dict(M=65535 * 32 + 1), LIMIT), (dict(D=(1 << 30) + 8, K=(1 << 30) + 8, ldx=(1 << 30) + 8), LIMIT)])
+    (dict(codes=Q + 8), ALIGN), (dict(gscale=S + 2), ALIGN), (dict(bias=P + 1), ALIGN), (dict(M=65535 * 32 + 1), LIMIT), (dict(D=(1 << 24) + 8, K=(1 << 24) + 8, ldx=(1 << 24) + 8), LIMIT)])
 def test_gemv(change, status):
     assert _gemv(**change) == status
-    assert L.nvfp4_gemv(P, 64, 2, 64, None, None, None, 0, None, None, T, 0, 40, None, None) == NULL
+    assert [L.nvfp4_gemv_workspace_bytes(m, 64, 0) for m in (0, 1, 2)] == [0, 0, 0] and L.nvfp4_gemv_workspace_bytes(3, 64, 0) == 3 * 512 + 64
+    assert L.nvfp4_gemv(P, 64, 2, 64, None, None, None, 0, None, None, T, 0, 40, None, None, 0, None) == NULL
 
 
 def _ck(codes=P, scales=Q, R=4, K=40):
