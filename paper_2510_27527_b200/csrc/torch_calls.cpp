@@ -56,7 +56,8 @@ void* vector(const at::Tensor& t, const char* where, const char* name, at::Scala
   return t.data_ptr();
 }
 
-void* bytes(const at::Tensor& t, const char* where, const char* name, int64_t at_least, c10::Device dev) {
+void* bytes(const at::Tensor& t, const char* where, const char* name, int64_t at_least, c10::Device dev, at::ScalarType type = at::kByte) {
+  TORCH_CHECK(t.scalar_type() == type, where, ": ", name, " is ", t.scalar_type(), ", not ", type);
   TORCH_CHECK(t.device() == dev && t.is_cuda() && t.is_contiguous(), where, ": ", name, " is on ", t.device(), ", not contiguous on ", dev);
   TORCH_CHECK((int64_t)t.nbytes() >= at_least, where, ": ", name, " has ", t.nbytes(), " bytes, too small for ", at_least);
   return t.data_ptr();
@@ -120,7 +121,7 @@ PyObject* gemv(PyObject*, Args a, Py_ssize_t n) {
   const bool sized = W.R > 0 && W.K > 0 && W.gs_mode >= 0 && W.gs_mode <= 2 && W.sf_layout >= 0 && W.sf_layout <= 1;  // (else the library refuses, or has nothing to do)
   W.codes = static_cast<uint8_t*>(bytes(tensor(a[1], where, "codes"), where, "codes", sized ? (int64_t)nvfp4_operand_codes_bytes(W.R, W.K) : 0, dev));
   W.sf = static_cast<uint8_t*>(bytes(tensor(a[2], where, "scales"), where, "scales", sized ? (int64_t)nvfp4_operand_sf_bytes(W.R, W.K, W.sf_layout) : 0, dev));
-  W.gscale = static_cast<float*>(bytes(tensor(a[3], where, "global scales"), where, "global scales", sized ? 4 * (int64_t)nvfp4_operand_gscale_count(W.R, W.K, W.gs_mode) : 0, dev));
+  W.gscale = static_cast<float*>(bytes(tensor(a[3], where, "global scales"), where, "global scales", sized ? 4 * (int64_t)nvfp4_operand_gscale_count(W.R, W.K, W.gs_mode) : 0, dev, at::kFloat));
   const void* bias = given(a[9]) ? vector(tensor(a[9], where, "bias"), where, "bias", at::kBFloat16, W.R, dev) : nullptr;
   int64_t n_out = 0;
   const int32_t *outl = nullptr, *keep = nullptr;

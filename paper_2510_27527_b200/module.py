@@ -161,3 +161,9 @@ class NVFP4Linear(torch.nn.Module):
         if self.bias is not None:
             y = y + self.bias
         return y if len(shape) == 2 else y.reshape(*shape[:-1], self.out_features)
+
+    def frozen(self):
+        """This layer for answering: its weights quantized now, once, and multiplied with a few BF16 tokens at a time (block.NVFP4FrozenLinear)."""
+        from .block import NVFP4FrozenLinear
+
+        return NVFP4FrozenLinear(self)
