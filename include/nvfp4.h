@@ -456,7 +456,7 @@ nvfp4_status nvfp4_osci_sparse_suppress(float* W, int64_t ldw, int64_t C, int64_
  *   Y        [M, N], leading dimension ldy, dtype y_dtype, 16-byte aligned rows. Columns from N on are left as they were.
  *   dev_status optional, see nvfp4_gemm (the waits are for copies of the weights).
  *   workspace nvfp4_gemv_workspace_bytes(M, D, n_out) bytes, 16-byte aligned (none for one and two tokens; may then be NULL).
- * Products of X and P * S_block are exact, sums are FP32 in an order that M does not change within 1 .. 2 and from 3 on; an element of X below 2^-28 of its token's
+ * Products of X and P * S_block are exact, sums are FP32 in an order that M does not change within 1 .. 2, within 3 .. 4 and from 5 on; an element of X below 2^-28 of its token's
  * largest in 128 columns may lose up to 2^-39 of that largest one. Non-finite elements of X give non-finite results of their token.
  * Errors: NULL / ENUM / SHAPE (K + n_out != D, K <= 0) / LIMIT (M > 2097120, D > 2^24, M D > 2^39) / ALIGN / WORKSPACE / ARCH; nothing is launched on an error.
  * --------------------------------------------------------------------------------------------------------- */
