@@ -83,10 +83,10 @@ __device__ __forceinline__ void ckpt8_decode(const uint2& q, f32x2 (&v)[4]) {
     v[i] = pair_of(f.x, f.y);
   }
 }
-// Stores the checkpoint of the eight elements v, whose largest finite-or-infinite magnitude is a, at column c of a row (c < ld, a multiple of
-// 8; elements past the row's end are 0). All four threads of a group call this together, whether they have elements or not; `store` says
-// whether this one writes.
-__device__ __forceinline__ void ckpt8_store(const f32x2 (&v)[4], float a, uint8_t* codes_row, uint8_t* scales_row, int c, bool store) {
+// Stores the checkpoint of the eight elements v, whose largest finite-or-infinite magnitude is a (elements past a row's end are 0). All four
+// threads of a group call this together, whether they have elements or not; `store` says whether this one writes, `first` whether it is the
+// group's first, which writes the scale.
+__device__ __forceinline__ void ckpt8_store(const f32x2 (&v)[4], float a, uint8_t* codes, uint8_t* scale, bool first, bool store) {
   a = fmaxf(a, 0.0f);  // (only NaN: 0)
   a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
   a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
@@ -110,8 +110,8 @@ __device__ __forceinline__ void ckpt8_store(const f32x2 (&v)[4], float a, uint8_
     q = ckpt8_encode(v, ckpt8_inverse(byte));
   }
   if (!store) return;
-  *reinterpret_cast<uint2*>(codes_row + c) = q;
-  if ((c & 31) == 0) scales_row[c >> 5] = (uint8_t)byte;
+  *reinterpret_cast<uint2*>(codes) = q;
+  if (first) *scale = (uint8_t)byte;
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -202,6 +202,22 @@ __device__ __forceinline__ Raw8<SRC> load8(const ActSrc& s, int64_t row, int c, 
   return r;
 }
 
+// Elements 8 i .. 8 i + 7 of a matrix without gaps between its rows (and, of a checkpoint, in its last groups).
+template <int SRC>
+__device__ __forceinline__ Raw8<SRC> load8_flat(const ActSrc& s, int64_t i) {
+  Raw8<SRC> r;
+  if constexpr (SRC == kSrcBf16) {
+    r.w = static_cast<const uint4*>(s.p)[i];
+  } else if constexpr (SRC == kSrcF32) {
+    r.lo = static_cast<const float4*>(s.p)[2 * i];
+    r.hi = static_cast<const float4*>(s.p)[2 * i + 1];
+  } else {
+    r.q = static_cast<const uint2*>(s.p)[i];
+    r.byte = s.scales[i >> 2];
+  }
+  return r;
+}
+
 // Eight values to a row of BF16 or FP32, those before D.
 __device__ __forceinline__ uint32_t bf16x2_of(float lo, float hi) {
   uint32_t w;
@@ -221,6 +237,9 @@ __device__ __forceinline__ void store_bf16x8(uint16_t* row, int c, int D, const 
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (c + i < D) row[c + i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+}
+__device__ __forceinline__ void store_bf16x8(uint16_t* at, const f32x2 (&v)[4]) {
+  *reinterpret_cast<uint4*>(at) = make_uint4(bf16x2_of(v[0]), bf16x2_of(v[1]), bf16x2_of(v[2]), bf16x2_of(v[3]));
 }
 __device__ __forceinline__ void store_f32x8(float* row, int c, int D, const f32x2 (&v)[4]) {
   const float2 a = values_of(v[0]), b = values_of(v[1]), d = values_of(v[2]), e = values_of(v[3]);

@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(kFwdThreadsOf<TPR>, kFwdThreadsPerSm<NV, TPR> 
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + lane) * 8;
-        ckpt8_store(v[i], amax[i], a.codes + row * ldc, a.scales + row * (ldc >> 5), c, c < ldc);
+        ckpt8_store(v[i], amax[i], a.codes + row * ldc + c, a.scales + row * (ldc >> 5) + (c >> 5), (c & 31) == 0, c < ldc);
       }
     }
     const float mean = group_sum<TPR>(sum_of(sum), slots[0][group], group, lane) * inv_D;

@@ -37,6 +37,25 @@ def test_pack_and_unpack(R, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("R,K", [(1, 32), (3, 64), (257, 96), (700, 1024), (3000, 2048)])
+def test_without_gaps(R, K, dtype):
+    """Matrices whose rows follow one another give what the same rows in a wider buffer give."""
+    from paper_2510_27527_b200 import binding as b
+
+    x = torch.from_numpy(inputs(R, K, 1, dtype)).cuda().to(dtype)
+    wide = torch.full((R, K + 16), float("nan"), dtype=dtype, device="cuda")
+    wide[:, :K] = x
+    ck, other = b.nvfp4_ckpt8_pack(x), b.nvfp4_ckpt8_pack(wide[:, :K])
+    assert torch.equal(ck.buf, other.buf)
+    if R * K <= 100000:
+        codes, scales, _ = O.ckpt8(host(x))
+        assert np.array_equal(ck.codes.cpu().numpy(), codes) and np.array_equal(ck.scales.cpu().numpy(), scales)
+    for out, code in ((torch.bfloat16, b.DT_BF16), (torch.float32, b.DT_F32)):
+        view, buf = guarded(R, K, out)
+        assert torch.equal(b.nvfp4_ckpt8_unpack(ck, code), b.nvfp4_ckpt8_unpack(ck, code, view)) and untouched(view, buf)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("scale", [1e-39, 1e-36, 1e-30, 1e30, 1e37])
 def test_scales_at_the_ends_of_the_range(scale, dtype):
     x = inputs(9, 70, 1, torch.bfloat16, hot=False) * np.float64(scale)

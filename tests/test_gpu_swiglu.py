@@ -96,6 +96,22 @@ def test_in_place_and_the_same_tensor_twice():
     assert torch.equal(H, b.nvfp4_swiglu_fwd(g, g.clone())[0])
 
 
+@pytest.mark.parametrize("save", [1, 2])
+@pytest.mark.parametrize("T,D", [(1, 32), (5, 96), (300, 2816), (77, 40)])
+def test_without_gaps(T, D, save):
+    """Matrices whose rows follow one another give what the same rows in wider buffers give."""
+    from paper_2510_27527_b200 import binding as b
+
+    wide = [device_rows(v, torch.bfloat16) for v in (inputs(T, D, 1), inputs(T, D, 2), synth.gradients(T, D, 3, 1e-3))]
+    flat = [v.contiguous() for v in wide]
+    H, saved = b.nvfp4_swiglu_fwd(flat[0], flat[1], save)
+    H2, saved2 = b.nvfp4_swiglu_fwd(wide[0], wide[1], save)
+    assert torch.equal(H, H2)
+    if save == 2:
+        assert torch.equal(saved.g8.buf, saved2.g8.buf) and torch.equal(saved.u8.buf, saved2.u8.buf)
+    assert all(torch.equal(p, q) for p, q in zip(b.nvfp4_swiglu_bwd(flat[2], saved), b.nvfp4_swiglu_bwd(wide[2], saved2)))
+
+
 def test_no_rows():
     from paper_2510_27527_b200 import binding as b
 
