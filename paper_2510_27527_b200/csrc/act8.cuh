@@ -188,18 +188,24 @@ struct ActSrc {
   const uint8_t* scales;  // of a checkpoint
   int64_t ld;
 };
+// The eight from an address on (and their group's scale), of which `left` belong to the row.
 template <int SRC>
-__device__ __forceinline__ Raw8<SRC> load8(const ActSrc& s, int64_t row, int c, int D) {
+__device__ __forceinline__ Raw8<SRC> load8_at(const void* p, const uint8_t* scale, int left) {
   Raw8<SRC> r;
   if constexpr (SRC == kSrcBf16) {
-    r.w = load_bf16x8(static_cast<const uint16_t*>(s.p) + row * s.ld, c, D);
+    r.w = load_bf16x8(static_cast<const uint16_t*>(p), 0, left);
   } else if constexpr (SRC == kSrcF32) {
-    load_f32x8(static_cast<const float*>(s.p) + row * s.ld, c, D, r.lo, r.hi);
-  } else {  // (codes past D are 0)
-    r.q = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(s.p) + row * s.ld + c);
-    r.byte = s.scales[row * (s.ld >> 5) + (c >> 5)];
+    load_f32x8(static_cast<const float*>(p), 0, left, r.lo, r.hi);
+  } else {  // (codes past the row's end are 0)
+    r.q = *static_cast<const uint2*>(p);
+    r.byte = *scale;
   }
   return r;
+}
+template <int SRC>
+__device__ __forceinline__ Raw8<SRC> load8(const ActSrc& s, int64_t row, int c, int D) {
+  constexpr int SIZE = SRC == kSrcF32 ? 4 : SRC == kSrcBf16 ? 2 : 1;
+  return load8_at<SRC>(static_cast<const uint8_t*>(s.p) + (row * s.ld + c) * SIZE, SRC == kSrcCkpt8 ? s.scales + row * (s.ld >> 5) + (c >> 5) : nullptr, D - c);
 }
 
 // Elements 8 i .. 8 i + 7 of a matrix without gaps between its rows (and, of a checkpoint, in its last groups).

@@ -107,15 +107,23 @@ __global__ void __launch_bounds__(kFwdThreadsOf<TPR>, kFwdThreadsPerSm<NV, TPR> 
   const float inv_D = 1.0f / (float)D;
   const f32x2 minus_one = pair_of(-1.0f);
   Raw8<SRC> next[NV];
+  int64_t row = (int64_t)blockIdx.x * GROUPS + group;
+  const int64_t step = (int64_t)gridDim.x * GROUPS;
+  // this thread's first elements of its rows; the pointers move from row to row
+  constexpr int SIZE = SRC == kSrcF32 ? 4 : 2;
+  const uint8_t* x = static_cast<const uint8_t*>(a.x.p) + (row * a.x.ld + lane * 8) * SIZE;
+  uint16_t* y = a.y + row * a.ldy + lane * 8;
+  uint8_t *codes = CK ? a.codes + row * ldc + lane * 8 : nullptr, *scales = CK ? a.scales + row * (ldc >> 5) + (lane >> 2) : nullptr;
+  const int64_t x_step = step * a.x.ld * SIZE, y_step = step * a.ldy, c_step = step * ldc, s_step = step * (ldc >> 5);
   auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + lane) * 8;
       next[i] = Raw8<SRC>{};
-      if (c < D && row < a.T) next[i] = load8<SRC>(a.x, row, c, D);
+      if (c < D && row < a.T) next[i] = load8_at<SRC>(x + (size_t)i * TPR * 8 * SIZE, nullptr, D - c);
     }
+    x += x_step;
   };
-  int64_t row = (int64_t)blockIdx.x * GROUPS + group;
   fetch(row);
   for (int j = group; j < 2 * NV; j += GROUPS) {
     const int c = ((j >> 1) * TPR + lane) * 8;
@@ -126,7 +134,7 @@ __global__ void __launch_bounds__(kFwdThreadsOf<TPR>, kFwdThreadsPerSm<NV, TPR> 
     for (int e = 0; e < 2; ++e) params[(((j & 1) * NV + (j >> 1)) * 2 + e) * TPR + lane] = make_ulonglong2(p[2 * e], p[2 * e + 1]);
   }
   __syncthreads();
-  for (; row < a.T; row += (int64_t)gridDim.x * GROUPS) {
+  for (; row < a.T; row += step) {
     f32x2 v[NV][4];
     float amax[NV];
     f32x2 sum = pair_of(0.0f);
@@ -137,13 +145,15 @@ __global__ void __launch_bounds__(kFwdThreadsOf<TPR>, kFwdThreadsPerSm<NV, TPR> 
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum = add2(sum, v[i][e]);
     }
-    fetch(row + (int64_t)gridDim.x * GROUPS);
+    fetch(row + step);
     if (CK) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + lane) * 8;
-        ckpt8_store(v[i], amax[i], a.codes + row * ldc + c, a.scales + row * (ldc >> 5) + (c >> 5), (c & 31) == 0, c < ldc);
+        ckpt8_store(v[i], amax[i], codes + i * TPR * 8, scales + i * TPR / 4, (lane & 3) == 0, c < ldc);
       }
+      codes += c_step;
+      scales += s_step;
     }
     const float mean = group_sum<TPR>(sum_of(sum), slots[0][group], group, lane) * inv_D;
     f32x2 sq = pair_of(0.0f);
@@ -177,8 +187,9 @@ __global__ void __launch_bounds__(kFwdThreadsOf<TPR>, kFwdThreadsPerSm<NV, TPR> 
         o[2 * e] = fma2(mul2(v[i][2 * e], pair_of(rstd)), g.x, b.x);
         o[2 * e + 1] = fma2(mul2(v[i][2 * e + 1], pair_of(rstd)), g.y, b.y);
       }
-      store_bf16x8(a.y + row * a.ldy, c, D, o);
+      store_bf16x8(y + i * TPR * 8, 0, D - c, o);
     }
+    y += y_step;
   }
 }
 
@@ -206,6 +217,17 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(NormBwdArgs a)
   Raw8<kSrcBf16> dy_next[NV];
   Raw8<SRC> x_next[NV];
   float2 st_next = make_float2(0.0f, 0.0f);
+  int64_t row = (int64_t)blockIdx.x * GROUPS + group;
+  const int64_t step = (int64_t)gridDim.x * GROUPS;
+  // this thread's first elements of its rows; the pointers move from row to row
+  constexpr int SIZE = SRC == kSrcF32 ? 4 : SRC == kSrcBf16 ? 2 : 1;
+  const uint8_t* dy = static_cast<const uint8_t*>(a.dy.p) + (row * a.dy.ld + lane * 8) * 2;
+  const uint8_t* x = static_cast<const uint8_t*>(a.x.p) + (row * a.x.ld + lane * 8) * SIZE;
+  const uint8_t* scales = SRC == kSrcCkpt8 ? a.x.scales + row * (a.x.ld >> 5) + (lane >> 2) : nullptr;
+  const float2* stats = a.stats + row;
+  const int dx_size = a.dx_f32 ? 4 : 2;
+  uint8_t* dx = static_cast<uint8_t*>(a.dx) + (row * a.lddx + lane * 8) * dx_size;
+  const int64_t dy_step = step * a.dy.ld * 2, x_step = step * a.x.ld * SIZE, s_step = step * (a.x.ld >> 5), dx_step = step * a.lddx * dx_size;
   auto fetch = [&](int64_t row) {
     if (row >= a.T) return;
 #pragma unroll
@@ -214,13 +236,16 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(NormBwdArgs a)
       dy_next[i] = Raw8<kSrcBf16>{};
       x_next[i] = Raw8<SRC>{};
       if (c < D) {
-        dy_next[i] = load8<kSrcBf16>(a.dy, row, c, D);
-        x_next[i] = load8<SRC>(a.x, row, c, D);
+        dy_next[i] = load8_at<kSrcBf16>(dy + i * TPR * 16, nullptr, D - c);
+        x_next[i] = load8_at<SRC>(x + i * TPR * 8 * SIZE, SRC == kSrcCkpt8 ? scales + i * TPR / 4 : nullptr, D - c);
       }
     }
-    st_next = a.stats[row];
+    st_next = *stats;
+    dy += dy_step;
+    x += x_step;
+    if (SRC == kSrcCkpt8) scales += s_step;
+    stats += step;
   };
-  int64_t row = (int64_t)blockIdx.x * GROUPS + group;
   fetch(row);
   if (group == 0) {
 #pragma unroll
@@ -236,7 +261,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(NormBwdArgs a)
   f32x2 dg[NV][4] = {}, db[NV][4] = {};
   const f32x2 minus_one = pair_of(-1.0f);
   int parity = 0;
-  for (; row < a.T; row += (int64_t)gridDim.x * GROUPS, parity ^= 1) {
+  for (; row < a.T; row += step, parity ^= 1) {
     f32x2 h[NV][4], xh[NV][4], s1 = pair_of(0.0f), s2 = s1;  // (past D dy and gamma are 0)
     const float2 st = st_next;
 #pragma unroll
@@ -253,7 +278,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(NormBwdArgs a)
         for (int e = 0; e < 4; ++e) xh[i][e] = mul2(fma2(minus_one, pair_of(st.x), xh[i][e]), pair_of(st.y));
       }
     }
-    fetch(row + (int64_t)gridDim.x * GROUPS);
+    fetch(row + step);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if ((i * TPR + lane) * 8 >= D) continue;
@@ -276,10 +301,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(NormBwdArgs a)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = mul2(add2(fma2(xh[i][e], c2, h[i][e]), c1), r);
       if (a.dx_f32)
-        store_f32x8(static_cast<float*>(a.dx) + row * a.lddx, c, D, o);
+        store_f32x8(reinterpret_cast<float*>(dx) + i * TPR * 8, 0, D - c, o);
       else
-        store_bf16x8(static_cast<uint16_t*>(a.dx) + row * a.lddx, c, D, o);
+        store_bf16x8(reinterpret_cast<uint16_t*>(dx) + i * TPR * 8, 0, D - c, o);
     }
+    dx += dx_step;
   }
   // the groups' sums: the upper half of them adds to the lower one until one is left
   __syncthreads();  // (gamma is done with)
