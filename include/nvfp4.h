@@ -458,7 +458,7 @@ nvfp4_status nvfp4_osci_sparse_suppress(float* W, int64_t ldw, int64_t C, int64_
  *   workspace nvfp4_gemv_workspace_bytes(M, D, n_out) bytes, 16-byte aligned (none for one and two tokens; may then be NULL).
  * Products of X and P * S_block are exact, sums are FP32 in an order that M does not change within 1 .. 2, within 3 .. 4 and from 5 on; an element of X below 2^-28 of its token's
  * largest in 128 columns may lose up to 2^-39 of that largest one. Non-finite elements of X give non-finite results of their token.
- * Errors: NULL / ENUM / SHAPE (K + n_out != D, K <= 0) / LIMIT (M > 2097120, D > 2^24, M D > 2^39) / ALIGN / WORKSPACE / ARCH; nothing is launched on an error.
+ * Errors: NULL / ENUM / SHAPE (K + n_out != D, K <= 0) / LIMIT (M > 2097120, D > 2^24, or more than 2^35 pieces of 128 columns of X) / ALIGN / WORKSPACE / ARCH; nothing is launched on an error.
  * --------------------------------------------------------------------------------------------------------- */
 size_t nvfp4_gemv_workspace_bytes(int64_t M, int64_t D, int64_t n_out);
 nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, const nvfp4_operand* W, const int32_t* keep_cols,
@@ -478,7 +478,7 @@ nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, c
  * The struct lives on the host, both arrays on the device; R and K are inputs and validated.
  *   nvfp4_ckpt8_pack    X [R, K] of x_dtype, leading dimension ldx, 16-byte aligned rows -> *out.
  *   nvfp4_ckpt8_unpack  *in -> X of x_dtype; columns of X from K on are left as they were.
- * Errors: NULL / ENUM / SHAPE / ALIGN / LIMIT (K > 2^24, or more than 2^42 elements) / ARCH; nothing is launched on an error.
+ * Errors: NULL / ENUM / SHAPE / ALIGN / LIMIT (K > 2^24, R > 2^38, or more than 2^42 elements) / ARCH; nothing is launched on an error.
  * --------------------------------------------------------------------------------------------------------- */
 typedef struct {
   uint8_t* codes;

@@ -101,7 +101,7 @@ struct CkptOut {
 };
 
 template <bool CK, bool FLAT>
-__global__ void __launch_bounds__(256) swiglu_fwd_kernel(ActSrc g, ActSrc u, int64_t T, int D, int ldc, uint16_t* __restrict__ h, int64_t ldh, CkptOut cg, CkptOut cu) {
+__global__ void __launch_bounds__(256) swiglu_fwd_kernel(ActSrc g, ActSrc u, int64_t T, int D, int ldc, uint16_t* h, int64_t ldh, CkptOut cg, CkptOut cu) {
   pdl_prologue();
   const int64_t n8 = CK ? ldc >> 3 : (D + 7) >> 3, total = T * n8;
   const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(256) swiglu_fwd_kernel(ActSrc g, ActSrc u, int
 }
 
 template <int SRC, bool FLAT>
-__global__ void __launch_bounds__(256) swiglu_bwd_kernel(ActSrc dh, ActSrc g, ActSrc u, int64_t T, int D, uint16_t* __restrict__ dg, int64_t lddg, uint16_t* __restrict__ du,
+__global__ void __launch_bounds__(256) swiglu_bwd_kernel(ActSrc dh, ActSrc g, ActSrc u, int64_t T, int D, uint16_t* dg, int64_t lddg, uint16_t* du,
                                                         int64_t lddu) {
   pdl_prologue();
   const int64_t n8 = (D + 7) >> 3, total = T * n8;
@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(256) swiglu_bwd_kernel(ActSrc dh, ActSrc g, Ac
   }
 }
 
-constexpr int64_t kMaxCols = (int64_t)1 << 24;  // columns are 32-bit in the kernels
+constexpr int64_t kMaxCols = (int64_t)1 << 24, kMaxRows = (int64_t)1 << 38;  // columns are 32-bit in the kernels; pieces do not pass 64 bits
 // CTAs of 256 threads for `pieces` pieces, nb a thread; 0: more than a grid has
 unsigned ctas(int64_t pieces, int nb = 1) {
   const int64_t n = (pieces + 256 * nb - 1) / (256 * nb);
@@ -212,7 +212,7 @@ nvfp4_status nvfp4_ckpt8_pack(const void* X, int32_t x_dtype, int64_t ldx, int64
   if (!out) return NVFP4_ERR_NULL;
   if (x_dtype < 0 || x_dtype > 1) return NVFP4_ERR_ENUM;
   if (R < 0 || K <= 0) return NVFP4_ERR_SHAPE;
-  if (K > kMaxCols) return NVFP4_ERR_LIMIT;
+  if (K > kMaxCols || R > kMaxRows) return NVFP4_ERR_LIMIT;
   nvfp4_status s = check_ckpt8(out, R, K);
   if (s != NVFP4_OK) return s;
   if (R == 0) return NVFP4_OK;
@@ -240,7 +240,7 @@ nvfp4_status nvfp4_ckpt8_unpack(const nvfp4_ckpt8* in, void* X, int32_t x_dtype,
   if (!in) return NVFP4_ERR_NULL;
   if (x_dtype < 0 || x_dtype > 1) return NVFP4_ERR_ENUM;
   if (in->R < 0 || in->K <= 0) return NVFP4_ERR_SHAPE;
-  if (in->K > kMaxCols) return NVFP4_ERR_LIMIT;
+  if (in->K > kMaxCols || in->R > kMaxRows) return NVFP4_ERR_LIMIT;
   nvfp4_status s = check_ckpt8(in, in->R, in->K);
   if (s != NVFP4_OK) return s;
   if (in->R == 0) return NVFP4_OK;
@@ -266,7 +266,7 @@ nvfp4_status nvfp4_ckpt8_unpack(const nvfp4_ckpt8* in, void* X, int32_t x_dtype,
 nvfp4_status nvfp4_swiglu_fwd(const void* G, int64_t ldg, const void* U, int64_t ldu, int64_t T, int64_t D, void* H, int64_t ldh, const nvfp4_ckpt8* g8,
                               const nvfp4_ckpt8* u8, void* stream) {
   if (T < 0 || D <= 0 || (g8 == nullptr) != (u8 == nullptr)) return NVFP4_ERR_SHAPE;
-  if (D > kMaxCols) return NVFP4_ERR_LIMIT;
+  if (D > kMaxCols || T > kMaxRows) return NVFP4_ERR_LIMIT;
   nvfp4_status s;
   if (g8 && ((s = check_ckpt8(g8, T, D)) != NVFP4_OK || (s = check_ckpt8(u8, T, D)) != NVFP4_OK)) return s;
   if (T == 0) return NVFP4_OK;
@@ -287,7 +287,7 @@ nvfp4_status nvfp4_swiglu_fwd(const void* G, int64_t ldg, const void* U, int64_t
 nvfp4_status nvfp4_swiglu_bwd(const void* dH, int64_t lddh, const void* G, int64_t ldg, const void* U, int64_t ldu, const nvfp4_ckpt8* g8, const nvfp4_ckpt8* u8,
                               int64_t T, int64_t D, void* dG, int64_t lddg, void* dU, int64_t lddu, void* stream) {
   if (T < 0 || D <= 0 || (g8 == nullptr) != (u8 == nullptr)) return NVFP4_ERR_SHAPE;
-  if (D > kMaxCols) return NVFP4_ERR_LIMIT;
+  if (D > kMaxCols || T > kMaxRows) return NVFP4_ERR_LIMIT;
   nvfp4_status s;
   if (g8 && ((s = check_ckpt8(g8, T, D)) != NVFP4_OK || (s = check_ckpt8(u8, T, D)) != NVFP4_OK)) return s;
   if (T == 0) return NVFP4_OK;

@@ -574,7 +574,8 @@ nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, c
   if (bad_matrix(X_bf16, ldx, D, 2) || bad_matrix(Y, ldy, W->R, y_dtype == NVFP4_DT_F32 ? 4 : 2) || !aligned(W->codes, 16) || !aligned(W->sf, 16) || !aligned(W->gscale, 4) ||
       !aligned(bias_bf16, 2) || (n_out > 0 && (!aligned(W_out, 16) || !aligned(keep_cols, 4) || !aligned(outlier_cols, 4))))
     return NVFP4_ERR_ALIGN;
-  if (M * ((D >> 7) + 4) > (int64_t)1 << 33) return NVFP4_ERR_LIMIT;  // (the grid that stages X)
+  const int64_t n_code_pairs = (nvfp4_padded_k(W->K) / 128 + 1) / 2, n_pairs = n_code_pairs + nvfp4_outlier_pad(n_out) / 64;
+  if (M * 2 * n_pairs > 16 * (int64_t)0x7FFFFFFF) return NVFP4_ERR_LIMIT;  // (the grid that stages X)
   if (M > 2 && (!workspace || !aligned(workspace, 16) || ws_bytes < nvfp4_gemv_workspace_bytes(M, D, n_out))) return NVFP4_ERR_WORKSPACE;
   if (!device_is_sm100()) return NVFP4_ERR_ARCH;
   GemvArgs a{};
@@ -599,8 +600,8 @@ nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, c
   a.y_f32 = y_dtype == NVFP4_DT_F32;
   a.ldy = ldy;
   a.n_codes = (int)(nvfp4_padded_k(W->K) / 128);
-  a.n_code_pairs = (a.n_codes + 1) / 2;
-  a.n_pairs = a.n_code_pairs + a.Kh / 64;
+  a.n_code_pairs = (int)n_code_pairs;
+  a.n_pairs = (int)n_pairs;
   a.dev_status = dev_status;
   CUtensorMap codes{}, outliers{};
   if (!encode_codes_map(&codes, W->codes, W->R, nvfp4_padded_k(W->K)) || (n_out > 0 && !encode_outliers_map(&outliers, W_out, W->R, a.Kh))) return NVFP4_ERR_CUDA;

@@ -69,6 +69,7 @@ int64_t ckpt8_bytes(int64_t R, int64_t K) {
   return R * (ld + ld / 32);
 }
 nvfp4_ckpt8 ckpt8(const at::Tensor& buf, const char* where, int64_t R, int64_t K, c10::Device dev) {
+  TORCH_CHECK(R >= 0 && K >= 0 && R <= ((int64_t)1 << 38) && K <= ((int64_t)1 << 24), where, ": a checkpoint of shape [", R, ", ", K, "]");  // (their product fits)
   TORCH_CHECK(buf.is_cuda() && buf.device() == dev, where, ": a checkpoint on ", buf.device(), ", not on ", dev.is_cuda() ? c10::str(dev) : "a CUDA device");
   TORCH_CHECK(buf.scalar_type() == at::kByte && buf.is_contiguous() && buf.numel() == ckpt8_bytes(R, K), where,
               ": no checkpoint for a matrix [", R, ", ", K, "] on ", dev, ": ", buf.scalar_type(), " ", buf.sizes(), " on ", buf.device());
@@ -173,7 +174,6 @@ PyObject* ckpt8_unpack(PyObject*, Args a, Py_ssize_t n) {
   const at::Tensor& buf = tensor(a[0], where, "the checkpoint");
   const c10::Device dev = buf.device();
   const int64_t R = whole(a[1]), K = whole(a[2]);
-  TORCH_CHECK(R >= 0 && K >= 0, where, ": a checkpoint of shape [", R, ", ", K, "]");
   const nvfp4_ckpt8 c = ckpt8(buf, where, R, K, dev);
   const at::ScalarType type = type_of(whole(a[3]), where);
   const Guard guard(dev);
