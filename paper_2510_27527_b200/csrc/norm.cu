@@ -96,7 +96,8 @@ struct NormFwdArgs {
   uint8_t *codes, *scales;
 };
 
-template <int SRC, bool CK, int NV, int TPR>
+// FULL: D is a multiple of eight, so that no piece of eight is cut short (1999 x 1000 forward 5.0 us against 5.5).
+template <int SRC, bool CK, int NV, int TPR, bool FULL>
 __global__ void __launch_bounds__(kFwdThreadsOf<TPR>, kFwdThreadsPerSm<NV, TPR> / kFwdThreadsOf<TPR>) norm_fwd_kernel(NormFwdArgs a) {
   pdl_prologue();
   constexpr int GROUPS = kFwdThreadsOf<TPR> / TPR;
@@ -120,7 +121,7 @@ __global__ void __launch_bounds__(kFwdThreadsOf<TPR>, kFwdThreadsPerSm<NV, TPR> 
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + lane) * 8;
       next[i] = Raw8<SRC>{};
-      if (c < D && row < a.T) next[i] = load8_at<SRC>(x + (size_t)i * TPR * 8 * SIZE, nullptr, D - c);
+      if (c < D && row < a.T) next[i] = load8_at<SRC>(x + (size_t)i * TPR * 8 * SIZE, nullptr, FULL ? 8 : D - c);
     }
     x += x_step;
   };
@@ -165,7 +166,7 @@ __global__ void __launch_bounds__(kFwdThreadsOf<TPR>, kFwdThreadsPerSm<NV, TPR> 
       if (c + 8 <= D) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) sq = fma2(v[i][e], v[i][e], sq);
-      } else {
+      } else if (!FULL) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float2 d = values_of(v[i][e]);
@@ -187,7 +188,7 @@ __global__ void __launch_bounds__(kFwdThreadsOf<TPR>, kFwdThreadsPerSm<NV, TPR> 
         o[2 * e] = fma2(mul2(v[i][2 * e], pair_of(rstd)), g.x, b.x);
         o[2 * e + 1] = fma2(mul2(v[i][2 * e + 1], pair_of(rstd)), g.y, b.y);
       }
-      store_bf16x8(y + i * TPR * 8, 0, D - c, o);
+      store_bf16x8(y + i * TPR * 8, 0, FULL ? 8 : D - c, o);
     }
     y += y_step;
   }
@@ -204,15 +205,15 @@ struct NormBwdArgs {
   float* partial;  // [CTA][dgamma, dbeta][columns up to a multiple of 8]
 };
 
-template <int SRC, int NV, int TPR>
+template <int SRC, int NV, int TPR, bool FULL>
 __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(NormBwdArgs a) {
   pdl_prologue();
   constexpr int GROUPS = kBwdThreads / TPR;
   extern __shared__ __align__(16) uint8_t smem[];
   const int group = threadIdx.x / TPR, lane = threadIdx.x % TPR, D = a.D;
   float2* const slots = reinterpret_cast<float2*>(smem) + group * (TPR / 32);  // and again kSlots further on
-  f32x2* const gamma = reinterpret_cast<f32x2*>(smem) + 2 * kSlots;       // [NV][4][TPR]
-  f32x2* const sums = gamma;                            // and at the end, GROUPS / 2 times [dgamma, dbeta][NV][4][TPR]
+  ulonglong2* const gamma = reinterpret_cast<ulonglong2*>(reinterpret_cast<f32x2*>(smem) + 2 * kSlots);  // [NV][2][TPR], four values each
+  f32x2* const sums = reinterpret_cast<f32x2*>(gamma);                            // and at the end, GROUPS / 2 times [dgamma, dbeta][NV][4][TPR]
   const float inv_D = 1.0f / (float)D;
   Raw8<kSrcBf16> dy_next[NV];
   Raw8<SRC> x_next[NV];
@@ -236,8 +237,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(NormBwdArgs a)
       dy_next[i] = Raw8<kSrcBf16>{};
       x_next[i] = Raw8<SRC>{};
       if (c < D) {
-        dy_next[i] = load8_at<kSrcBf16>(dy + i * TPR * 16, nullptr, D - c);
-        x_next[i] = load8_at<SRC>(x + i * TPR * 8 * SIZE, SRC == kSrcCkpt8 ? scales + i * TPR / 4 : nullptr, D - c);
+        dy_next[i] = load8_at<kSrcBf16>(dy + i * TPR * 16, nullptr, FULL ? 8 : D - c);
+        x_next[i] = load8_at<SRC>(x + i * TPR * 8 * SIZE, SRC == kSrcCkpt8 ? scales + i * TPR / 4 : nullptr, FULL ? 8 : D - c);
       }
     }
     st_next = *stats;
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(NormBwdArgs a)
       f32x2 g[4] = {};
       if (c < D) params8(a.gamma, a.params_f32, c, D, g);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) gamma[(i * 4 + e) * TPR + lane] = g[e];
+      for (int e = 0; e < 2; ++e) gamma[(i * 2 + e) * TPR + lane] = make_ulonglong2(g[2 * e], g[2 * e + 1]);
     }
   }
   __syncthreads();
@@ -282,11 +283,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(NormBwdArgs a)
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if ((i * TPR + lane) * 8 >= D) continue;
+      const ulonglong2 g01 = gamma[i * 2 * TPR + lane], g23 = gamma[(i * 2 + 1) * TPR + lane];
+      const f32x2 gam[4] = {g01.x, g01.y, g23.x, g23.y};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         dg[i][e] = fma2(h[i][e], xh[i][e], dg[i][e]);
         db[i][e] = add2(h[i][e], db[i][e]);
-        h[i][e] = mul2(h[i][e], gamma[(i * 4 + e) * TPR + lane]);
+        h[i][e] = mul2(h[i][e], gam[e]);
         s1 = add2(s1, h[i][e]);
         s2 = fma2(h[i][e], xh[i][e], s2);
       }
@@ -301,9 +304,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(NormBwdArgs a)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = mul2(add2(fma2(xh[i][e], c2, h[i][e]), c1), r);
       if (a.dx_f32)
-        store_f32x8(reinterpret_cast<float*>(dx) + i * TPR * 8, 0, D - c, o);
+        store_f32x8(reinterpret_cast<float*>(dx) + i * TPR * 8, 0, FULL ? 8 : D - c, o);
       else
-        store_bf16x8(reinterpret_cast<uint16_t*>(dx) + i * TPR * 8, 0, D - c, o);
+        store_bf16x8(reinterpret_cast<uint16_t*>(dx) + i * TPR * 8, 0, FULL ? 8 : D - c, o);
     }
     dx += dx_step;
   }
@@ -402,7 +405,7 @@ cudaError_t launch_norm_fwd(const NormFwdArgs& a, cudaStream_t st) {
   return with_fwd_shape(a.D, [&](auto nv, auto tpr) {
     constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value, THREADS = kFwdThreadsOf<TPR>, GROUPS = THREADS / TPR;
     constexpr size_t smem = (size_t)2 * NV * 2 * TPR * sizeof(ulonglong2);
-    auto kernel = norm_fwd_kernel<SRC, CK, NV, TPR>;
+    auto kernel = a.D % 8 ? norm_fwd_kernel<SRC, CK, NV, TPR, false> : norm_fwd_kernel<SRC, CK, NV, TPR, true>;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem + 1024);
     if (e != cudaSuccess) return e;
     const int64_t ctas = std::min<int64_t>((a.T + GROUPS - 1) / GROUPS, (int64_t)device_sm_count() * (kFwdThreadsPerSm<NV, TPR> / THREADS));
@@ -422,7 +425,7 @@ cudaError_t launch_norm_bwd(const NormBwdArgs& a, int ctas, cudaStream_t st) {
   return with_shape<2>(a.D, [&](auto nv, auto tpr) {
     constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value, GROUPS = kBwdThreads / TPR;
     constexpr size_t smem = (2 * kSlots + (size_t)GROUPS * NV * 4 * TPR) * sizeof(f32x2);  // slots; gamma, or the sums of half the groups
-    auto kernel = norm_bwd_kernel<SRC, NV, TPR>;
+    auto kernel = a.D % 8 ? norm_bwd_kernel<SRC, NV, TPR, false> : norm_bwd_kernel<SRC, NV, TPR, true>;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return e;
     return launch_kernel(kernel, dim3((unsigned)ctas), dim3(kBwdThreads), smem, st, a);
