@@ -8,7 +8,9 @@
  *         Y = Q1(X) Q2(W)^T,   dX = Q3(dY) Q4(W-hat),   dW = Q5(dY^T) Q6(X-hat),
  *     where backward re-quantizes the dequantized forward operands X-hat, W-hat;
  *   - OutControl's split (Sec. 4.2, without the Hadamard factors): a static set of outlier channels of X / W
- *     stays in BF16 and goes through high-precision products.
+ *     stays in BF16 and goes through high-precision products;
+ *   - what stands around the linears of a block: products of a few tokens with quantized weights, layer norm, SwiGLU, and
+ *     the 8-bit activation checkpoints that both keep for backward.
  *
  * Conventions, valid for every entry point unless stated otherwise:
  *   - All data pointers are DEVICE pointers owned by the caller. The library never allocates, frees or

@@ -114,9 +114,11 @@ class NVFP4FrozenLinear(torch.nn.Module):
     def __init__(self, layer: NVFP4Linear):
         super().__init__()
         self.in_features, self.out_features = layer.in_features, layer.out_features
+        if not layer.weight.is_cuda or layer.weight.dtype != torch.bfloat16:
+            raise RuntimeError(f"NVFP4FrozenLinear: weights of {layer.weight.dtype} on {layer.weight.device}, not BF16 on a CUDA device")
         cfg = dataclasses.replace(layer.cfg, dev_status=None, y_dtype=B.DT_BF16)
         self.gs_mode, self.n_out = cfg.gs_mode, cfg.n_out
-        with torch.no_grad():  # the call that quantizes the weights in training, on one token
+        with torch.no_grad(), torch.cuda.device(layer.weight.device):  # the call that quantizes the weights in training, on one token
             _, saved = B.nvfp4_linear_fwd(torch.ones((1, self.in_features), dtype=torch.bfloat16, device=layer.weight.device), layer.weight.detach(), cfg)
             index = saved.index if self.n_out else (None, None)
             for name, t in (("codes", saved.qw.codes), ("scales", saved.qw.sf), ("global_scales", saved.qw.gscale), ("outlier_cols", index[0]), ("keep_cols", index[1]),
@@ -142,16 +144,18 @@ class NVFP4FrozenLinear(torch.nn.Module):
 
 class NVFP4MLP(torch.nn.Module):
     """down(silu(gate(n)) * up(n)), n = norm(x): the MLP of a pre-norm block with NVFP4 linears (the caller adds the residual). `cfg` configures the
-    gate and up projections, `down_cfg` the down projection (default: cfg; outlier channels are those of the layer's own input width)."""
+    gate and up projections, `down_cfg` the down projection (default: cfg without its outlier channels, which are channels of x)."""
 
     def __init__(self, hidden: int, ffn: int, cfg: B.LayerConfig | None = None, down_cfg: B.LayerConfig | None = None, checkpoint: bool = True, eps: float = 1e-5,
                  norm_bias: bool = True, norm_dtype: torch.dtype = torch.bfloat16, device="cuda"):
         super().__init__()
         self.checkpoint = checkpoint
+        if down_cfg is None and cfg is not None:
+            down_cfg = dataclasses.replace(cfg, outliers=None) if cfg.n_out else cfg
         self.norm = NVFP4LayerNorm(hidden, eps, norm_bias, checkpoint, norm_dtype, device)
         self.gate = NVFP4Linear(hidden, ffn, cfg=cfg, device=device)
         self.up = NVFP4Linear(hidden, ffn, cfg=cfg, device=device)
-        self.down = NVFP4Linear(ffn, hidden, cfg=down_cfg if down_cfg is not None else cfg, device=device)
+        self.down = NVFP4Linear(ffn, hidden, cfg=down_cfg, device=device)
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         n = self.norm(x)

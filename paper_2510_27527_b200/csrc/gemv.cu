@@ -1,20 +1,30 @@
 // nvfp4_gemv: a few tokens times quantized weights, Y[m, n] = sum_k X[m, k] (P Sb Sg)[n, k] (+ the outlier channels' BF16 product, + bias), the
 // product of token-by-token answering. X stays in BF16 (nothing about it is quantized); the weights are read once, 0.5625 bytes each.
 //
-// The work is reading the weights, so all else is kept off their way. A warp takes 16 weight rows x 128 k at a time, 16 bytes (32 codes) of two
-// rows per lane, and multiplies them on the tensor cores (mma m16n8k16: 8 tokens cost what one costs): E2M1 pairs become FP16 pairs in one
-// conversion each, times the block scale exactly (P * Sb has at most 7 significant bits and lies within FP16's normal range). Which k stand
+// The work is reading the weights, so all else is kept off their way. A warp takes 32 weight rows x 128 k at a time, 16 bytes (32 codes) of four
+// rows per lane, and multiplies them on the tensor cores (mma m16n8k16: 8 tokens cost what one costs; tcgen05 would want codes that somebody has
+// expanded into shared memory, or X in FP4): E2M1 pairs become FP16 pairs in one conversion each, times the block scale exactly (P * Sb has at
+// most 7 significant bits and lies within FP16's normal range). Those multiplications share a pipe with the matrix instructions: in a loop of
+// its own two words of codes take 34 cycles of a sub-partition with them, 23 without (conversions 16, matrix instructions 16). Up to two tokens,
+// where an instruction's other columns are free, sums of one block each are scaled instead (SEP below). Which k stand
 // in which slot of an instruction is free as long as both operands agree, so the codes are used as they lie in memory and X is staged in
 // shared memory in that order. FP16 also holds X: a token's 128 values are scaled by the power of two that brings their largest magnitude to
 // [2^14, 2^15); a BF16 value has 8 significant bits, so the scaling is exact for all down to 2^-28 of the largest, and what is below loses less
 // than 2^-39 of it. Every 128 k the FP32 result of the instructions is added to FP32 sums with the product of that power of two and the
 // weights' global scale, which is constant there in every scale mode.
 // The outlier channels go through BF16 instructions, 32 of them per step, with the same rows.
+//
 // A CTA takes a 128-row tile, because that is whose scale bytes lie together, 256 k at a time: one tensor copy of 128 bytes of its rows (128-byte
 // swizzle), one of their scales, three or four of them in flight. One warp has them brought; eight take 32 rows and one of the
-// two halves of the 256 k each. The k axis is split over the CTAs of a cluster as well. At the end every warp sends its
-// sums to the shared memory of the CTA that finishes these rows, which adds them up in a fixed order, one that M does not change.
-// Waits are for copies alone, and bounded.
+// two halves of the 256 k each. The k axis is split over the CTAs of a cluster as well, whose sums are read through distributed
+// shared memory and added in a fixed order. Waits are for copies alone, and bounded.
+//
+// Measured (us, weights from HBM, replayed from a graph; the weights alone at the copy bandwidth in brackets): 1024 x 1024 times one token 3.0
+// (0.1), 4096 x 4096 5.9 (1.5), 8192 x 8192 11.2 (5.8); times 8 with 1x128 outer blocks 15.5, times 16 17.6, times 32 29; 14336 x 4096 times
+// 16 18.1 (5.2). What bounds it: for one token the chain of a warp's conversions and matrix instructions at 0.45 of the issue slots, and what a
+// short kernel begins and ends with (2 us until X is staged and the first weights are there, 1.5 for the cluster's sums); for more tokens the pipe
+// above. Measured and not better: rows through each warp's own ring of asynchronous copies (14.6 for 8192 x 8192 times one), three CTAs
+// to an SM (13.6), more CTAs than fit at once (16.6), X staged by every CTA for 16 tokens (24.8 against 17.6).
 #include "../../include/nvfp4.h"
 
 #include "act8.cuh"

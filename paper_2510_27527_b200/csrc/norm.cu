@@ -6,6 +6,13 @@
 // work on this one; the parameters stay in registers (forward) or, as FP32, in shared memory (backward, whose registers hold the two sums of
 // the thread's columns). At the end the groups of a CTA add their column sums up in shared memory, the CTAs through a small FP32 matrix that a
 // second launch sums. Every sum has a fixed order.
+//
+// Measured (us, inputs from HBM, replayed from a graph; in brackets the share of the copy bandwidth), forward / backward: 16384 x 1024 BF16 14.2
+// (0.72) / 24.3 (0.64), with the checkpoint 17.7 (0.73) / 22.7 (0.57), 4096 x 4096 so 19.4 (0.67) / 24.2 (0.54), 2048 x 8192 so 20.7 (0.63) / 26.4
+// (0.49), FP32 4095 x 4096 19.4 (0.80) / 34.0 (0.76). Instructions bound it (0.55 - 0.57 of the issue slots, two thirds of them arithmetic in
+// pairs), with the chain through a row's sums; of backward about 4 us are the second launch. Registers decide the rest: forward gains from
+// warps (FP32 4095 x 4096 22.2 with 512 threads on an SM, 19.6 with 1024), backward loses more by spilling than they bring (16384 x 1024 23.6
+// with 128 registers, 52 with 85), and a row in one warp there holds too many sums (41.7).
 #include "../../include/nvfp4.h"
 
 #include "act8.cuh"
@@ -82,6 +89,13 @@ __device__ __forceinline__ float2 group_sum2(float x, float y, float2* slot, int
     const float other = __shfl_xor_sync(0xFFFFFFFFu, v, 16);
     return upper ? make_float2(other, v) : make_float2(v, other);
   }
+}
+
+__device__ __forceinline__ void store_grad(void* out, int f32, int c, float v) {  // (a gradient of a parameter may lie on any address of its type)
+  if (f32)
+    static_cast<float*>(out)[c] = v;
+  else
+    static_cast<uint16_t*>(out)[c] = (uint16_t)bf16x2_of(v, 0.0f);
 }
 
 struct NormFwdArgs {
@@ -202,7 +216,9 @@ struct NormBwdArgs {
   const float2* stats;
   void* dx;
   int64_t lddx;
-  float* partial;  // [CTA][dgamma, dbeta][columns up to a multiple of 8]
+  float* partial;  // [CTA][dgamma, dbeta][columns up to a multiple of 8]; unused by a single CTA, which writes the gradients
+  void *dgamma, *dbeta;
+  int grads_f32;
 };
 
 template <int SRC, int NV, int TPR, bool FULL>
@@ -333,6 +349,20 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(NormBwdArgs a)
     __syncthreads();
   }
   if (group != 0) return;
+  if (gridDim.x == 1) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * TPR + lane) * 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (c + e >= D) continue;
+        const float2 g = values_of(dg[i][e >> 1]), b = values_of(db[i][e >> 1]);
+        store_grad(a.dgamma, a.grads_f32, c + e, e & 1 ? g.y : g.x);
+        if (a.has_beta) store_grad(a.dbeta, a.grads_f32, c + e, e & 1 ? b.y : b.x);
+      }
+    }
+    return;
+  }
   const int Dp = (D + 7) & ~7;
   float* out = a.partial + (size_t)blockIdx.x * 2 * Dp;
 #pragma unroll
@@ -363,11 +393,7 @@ __global__ void __launch_bounds__(1024) norm_bwd_finish_kernel(const float* __re
   float t = 0.0f;
 #pragma unroll
   for (int w = 0; w < 32; ++w) t += red[w][lane];
-  void* out = blockIdx.y ? dbeta : dgamma;
-  if (f32)
-    static_cast<float*>(out)[c] = t;
-  else
-    static_cast<uint16_t*>(out)[c] = (uint16_t)bf16x2_of(t, 0.0f);
+  store_grad(blockIdx.y ? dbeta : dgamma, f32, c, t);
 }
 
 // The shape of a row's group: as few threads as hold the row in MOST vectors each (three in forward, two in backward, whose registers hold
@@ -416,7 +442,8 @@ cudaError_t launch_norm_fwd(const NormFwdArgs& a, cudaStream_t st) {
 int bwd_ctas(int64_t T, int D) {
   return with_shape<2>(D, [&](auto, auto tpr) {
     constexpr int GROUPS = kBwdThreads / decltype(tpr)::value;
-    return (int)std::min<int64_t>((T + GROUPS - 1) / GROUPS, kBwdCtas);
+    // (up to two rows a group, one CTA without the second launch: us from Python, 16 x 1024 7.4 against 10.8)
+    return T <= 2 * GROUPS ? 1 : (int)std::min<int64_t>((T + GROUPS - 1) / GROUPS, kBwdCtas);
   });
 }
 
@@ -509,9 +536,13 @@ nvfp4_status nvfp4_layernorm_bwd(const void* dY, int64_t lddy, const void* X, in
     a.dx = dX;
     a.lddx = lddx;
     a.partial = static_cast<float*>(workspace);
+    a.dgamma = dgamma;
+    a.dbeta = dbeta;
+    a.grads_f32 = dparam_dtype == NVFP4_DT_F32;
     const cudaError_t e = x8 ? launch_norm_bwd<kSrcCkpt8>(a, ctas, st)
                              : x_dtype == NVFP4_DT_F32 ? launch_norm_bwd<kSrcF32>(a, ctas, st) : launch_norm_bwd<kSrcBf16>(a, ctas, st);
     if (e != cudaSuccess || cudaGetLastError() != cudaSuccess) return NVFP4_ERR_CUDA;
+    if (ctas == 1) return NVFP4_OK;
   }
   launch_kernel(norm_bwd_finish_kernel, dim3((unsigned)((D + 31) / 32), dbeta ? 2u : 1u), dim3(1024), 0, st, static_cast<const float*>(workspace), T > 0 ? ctas : 0, (int)D,
                 (int)(dparam_dtype == NVFP4_DT_F32), dgamma, dbeta);

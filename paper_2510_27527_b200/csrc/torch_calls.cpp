@@ -3,8 +3,8 @@
 // device), allocates from torch's caching allocator what the caller has not brought, and makes the library call on the current stream of the
 // tensors' device, whichever device is current.
 //
-// As with NVFP4Linear's node, what it replaces is host time: the same calls through ctypes take 12 to 21 us each, which is all of the time
-// of a call on a few tokens.
+// As with NVFP4Linear's node, what it replaces is host time, which is all of the time of a call on a few tokens: through ctypes a product, a norm
+// or a SwiGLU of a few tokens took 12.5 to 13.3 us from Python, this way 4.5 to 5.5.
 #include "torch_common.h"
 
 #include <c10/cuda/CUDAGuard.h>

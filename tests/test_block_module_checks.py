@@ -20,3 +20,26 @@ def test_shapes_and_types():
             swiglu(a, b)
     with pytest.raises(RuntimeError, match="CUDA device"):
         swiglu(x, x)
+
+
+def test_only_weights_on_a_device_are_frozen():
+    from paper_2510_27527_b200.block import NVFP4MLP
+    from paper_2510_27527_b200.module import NVFP4Linear
+
+    with pytest.raises(RuntimeError, match="CUDA device"):
+        NVFP4Linear(64, 32, device="cpu").frozen()
+    with pytest.raises(RuntimeError, match="CUDA device"):
+        NVFP4MLP(64, 128, device="cpu").frozen()
+
+
+def test_an_mlps_outlier_channels_are_its_inputs():
+    import numpy as np
+
+    from paper_2510_27527_b200 import binding as b
+    from paper_2510_27527_b200.block import NVFP4MLP
+
+    cfg = b.LayerConfig(outliers=np.array([3, 60]), rht=True, seed=7)
+    m = NVFP4MLP(64, 128, cfg, device="cpu")
+    assert m.gate.cfg is cfg and m.up.cfg is cfg and m.down.cfg.n_out == 0 and m.down.cfg.rht and m.down.cfg.seed == 7
+    other = b.LayerConfig(outliers=np.array([100]))
+    assert NVFP4MLP(64, 128, cfg, other, device="cpu").down.cfg is other

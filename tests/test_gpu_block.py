@@ -190,6 +190,24 @@ def test_answering_with_a_trained_mlp(tokens):
         copy.deepcopy(frozen).half()
 
 
+def test_mlp_with_outlier_channels():
+    """The gate and up projections' outlier channels are channels of the normed input; frozen, they are multiplied in BF16."""
+    m = mlp(outliers=np.array([0, 17, 199]), rht=True)
+    x = torch.from_numpy(inputs(64, 200, 1)).cuda().bfloat16().requires_grad_()
+    y = m(x)
+    y.backward(torch.ones_like(y))
+    assert all(torch.isfinite(p.grad).all() for p in (x, *m.parameters()))
+    frozen = m.frozen()
+    assert frozen.gate.n_out == 3 and frozen.down.n_out == 0
+    only = torch.zeros(4, 200, device="cuda").bfloat16()  # the other channels' codes are multiplied by zero
+    only[:, [0, 17, 199]] = torch.randn(4, 3, device="cuda").bfloat16()
+    with torch.no_grad():
+        got = host(frozen.gate(only))
+    w = host(m.gate.weight)
+    want, absdot = host(only) @ w.T, np.abs(host(only)) @ np.abs(w).T
+    assert np.all(np.abs(got - want) <= 2.0 ** -15 * absdot + BF16 * np.abs(want))
+
+
 def test_training_step_captured():
     """Forward and backward of the MLP in a CUDA graph give what eager calls with the same keys give."""
     m = mlp()
