@@ -125,12 +125,12 @@ class NVFP4FrozenLinear(torch.nn.Module):
                             ("outlier_weight", saved.W_out), ("bias", None if layer.bias is None else layer.bias.detach())):
                 self.register_buffer(name, None if t is None else t.clone())
 
-    def _apply(self, fn, recurse=True):  # a change of type is for other modules' parameters: the operand's arrays have one each
-        kinds = {n: b.dtype for n, b in self._buffers.items() if b is not None}
+    def _apply(self, fn, recurse=True):  # (a model's change of type is not for the operand's arrays, which have one each; one of device is)
+        before = {n: b for n, b in self._buffers.items() if b is not None}
         super()._apply(fn, recurse)
-        for n, dtype in kinds.items():
-            if self._buffers[n].dtype != dtype:
-                raise RuntimeError(f"NVFP4FrozenLinear: {n} is {dtype} and cannot become {self._buffers[n].dtype}")
+        for n, b in before.items():
+            if self._buffers[n].dtype != b.dtype:
+                self._buffers[n] = b.to(self._buffers[n].device)
         return self
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
