@@ -11,7 +11,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding as B
-from .module import NVFP4Linear
+from .module import NVFP4Linear, _needs_function, _wants_grad
 
 
 def _rows(x: torch.Tensor, features: int, where: str) -> torch.Tensor:
@@ -30,12 +30,18 @@ def _bf16(x: torch.Tensor) -> torch.Tensor:
     return x if x.dtype == torch.bfloat16 else x.to(torch.bfloat16)
 
 
+def _save(ctx, checkpoint: bool) -> int:
+    """What a call keeps. (Nothing where it goes through its function for a trace alone.)"""
+    return B.SAVE_NOTHING if not any(ctx.needs_input_grad) else B.SAVE_CKPT8 if checkpoint else B.SAVE_INPUT
+
+
 class _LayerNormFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gamma, beta, eps, checkpoint):
-        y, s = B.nvfp4_layernorm_fwd(x, gamma, beta, eps, B.SAVE_CKPT8 if checkpoint else B.SAVE_INPUT)
-        ctx.save_for_backward(gamma, s.stats, x if s.x8 is None else s.x8.buf)
-        ctx.saved = (s.T, s.D, s.x_dtype, s.has_beta, checkpoint)
+        y, s = B.nvfp4_layernorm_fwd(x, gamma, beta, eps, _save(ctx, checkpoint))
+        if s is not None:
+            ctx.save_for_backward(gamma, s.stats, x if s.x8 is None else s.x8.buf)
+            ctx.saved = (int(s.T), int(s.D), s.x_dtype, s.has_beta, checkpoint)  # (under jit.trace sizes are tensors)
         return y
 
     @staticmethod
@@ -51,9 +57,10 @@ class _LayerNormFn(torch.autograd.Function):
 class _SwigluFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, g, u, checkpoint):
-        h, s = B.nvfp4_swiglu_fwd(g, u, B.SAVE_CKPT8 if checkpoint else B.SAVE_INPUT)
-        ctx.save_for_backward(*((g, u) if s.g8 is None else (s.g8.buf, s.u8.buf)))
-        ctx.saved = (s.T, s.D, checkpoint)
+        h, s = B.nvfp4_swiglu_fwd(g, u, _save(ctx, checkpoint))
+        if s is not None:
+            ctx.save_for_backward(*((g, u) if s.g8 is None else (s.g8.buf, s.u8.buf)))
+            ctx.saved = (int(s.T), int(s.D), checkpoint)
         return h
 
     @staticmethod
@@ -64,20 +71,36 @@ class _SwigluFn(torch.autograd.Function):
         return *B.nvfp4_swiglu_bwd(_rows(_bf16(dh), D, "swiglu"), s), None
 
 
-def _wants_grad(*tensors) -> bool:
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+def _gemv(x, codes, scales, global_scales, outlier_cols, keep_cols, outlier_weight, bias, N, K, gs_mode):
+    W = B.Operand(codes, scales, global_scales, N, K, gs_mode, B.SF_TILED128x4)
+    return B.nvfp4_gemv(x, W, B.DT_BF16, bias, None if outlier_cols is None else (outlier_cols, keep_cols), outlier_weight)
 
 
-@torch.compiler.disable  # (a trace would not see what the library writes)
+class _FrozenFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, *args):
+        return _gemv(*args)
+
+    @staticmethod
+    def backward(ctx, dy):
+        raise RuntimeError("NVFP4FrozenLinear has no gradient")
+
+
+@torch.compiler.disable
+def _frozen(*args):
+    return _FrozenFn.apply(*args) if _needs_function(*args[:8]) else _gemv(*args)
+
+
+@torch.compiler.disable  # (a compiler would not see what the library writes)
 def _layer_norm(x, gamma, beta, eps, checkpoint):
-    if _wants_grad(x, gamma, beta):
+    if _needs_function(x, gamma, beta):
         return _LayerNormFn.apply(x, gamma, beta, eps, checkpoint)
     return B.nvfp4_layernorm_fwd(x, gamma, beta, eps, B.SAVE_NOTHING)[0]
 
 
 @torch.compiler.disable
 def _swiglu(g, u, checkpoint):
-    if _wants_grad(g, u):
+    if _needs_function(g, u):
         return _SwigluFn.apply(g, u, checkpoint)
     return B.nvfp4_swiglu_fwd(g, u, B.SAVE_NOTHING)[0]
 
@@ -137,8 +160,8 @@ class NVFP4FrozenLinear(torch.nn.Module):
         if _wants_grad(x):
             raise RuntimeError("NVFP4FrozenLinear has no gradient: use it under torch.no_grad()")
         rows = _rows(_bf16(x), self.in_features, "NVFP4FrozenLinear")
-        W = B.Operand(self.codes, self.scales, self.global_scales, self.out_features, self.in_features - self.n_out, self.gs_mode, B.SF_TILED128x4)
-        y = B.nvfp4_gemv(rows, W, B.DT_BF16, self.bias, (self.outlier_cols, self.keep_cols) if self.n_out else None, self.outlier_weight)
+        y = _frozen(rows, self.codes, self.scales, self.global_scales, self.outlier_cols, self.keep_cols, self.outlier_weight, self.bias, self.out_features,
+                    self.in_features - self.n_out, self.gs_mode)
         return y if x.dim() == 2 else y.reshape(*x.shape[:-1], self.out_features)
 
 
@@ -179,6 +202,6 @@ class NVFP4FrozenMLP(torch.nn.Module):
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         if _wants_grad(x):
             raise RuntimeError("NVFP4FrozenMLP has no gradient: use it under torch.no_grad()")
-        n = B.nvfp4_layernorm_fwd(_rows(x, self.features, "NVFP4FrozenMLP"), self.norm_weight, self.norm_bias, self.eps, B.SAVE_NOTHING)[0]
-        y = self.down(B.nvfp4_swiglu_fwd(self.gate(n), self.up(n), B.SAVE_NOTHING)[0])
+        n = _layer_norm(_rows(x, self.features, "NVFP4FrozenMLP"), self.norm_weight, self.norm_bias, self.eps, False)
+        y = self.down(_swiglu(self.gate(n), self.up(n), False))
         return y if x.dim() == 2 else y.reshape(x.shape)

@@ -100,12 +100,16 @@ def _plain(x: torch.Tensor, weight: torch.Tensor) -> bool:
             and not torch._C._is_tracing() and not torch._C._are_functorch_transforms_active())
 
 
-def _needs_function(x: torch.Tensor, weight: torch.Tensor) -> bool:
-    """Whether a call that the native node does not serve has to go through the autograd function: a gradient can be asked for, an input may
-    carry a forward-mode tangent or be a transform's (which the function refuses), or a trace is being recorded (which sees the function, but
-    not what the library writes). Else it goes to the library at once (48 instead of 55 us on 77 tokens)."""
-    return ((torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad)) or forward_ad._current_level >= 0 or torch.jit.is_tracing()
-            or torch._C._are_functorch_transforms_active())
+def _wants_grad(*tensors) -> bool:
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def _needs_function(*tensors) -> bool:
+    """Whether a call (one that the native node does not serve, or one of the steps around the linears) has to go through its autograd function:
+    a gradient can be asked for, an input may carry a forward-mode tangent or be a transform's (which the function refuses), or a trace is being
+    recorded (which sees the function, but not what the library writes). Else it goes to the library at once (a linear on 77 tokens: 48 instead
+    of 55 us)."""
+    return _wants_grad(*tensors) or forward_ad._current_level >= 0 or torch.jit.is_tracing() or torch._C._are_functorch_transforms_active()
 
 
 class _NVFP4LinearFn(torch.autograd.Function):
