@@ -8,10 +8,11 @@
 // its own two words of codes take 34 cycles of a sub-partition with them, 23 without (conversions 16, matrix instructions 16). Up to two tokens,
 // where an instruction's other columns are free, sums of one block each are scaled instead (SEP below). Which k stand
 // in which slot of an instruction is free as long as both operands agree, so the codes are used as they lie in memory and X is staged in
-// shared memory in that order. FP16 also holds X: a token's 128 values are scaled by the power of two that brings their largest magnitude to
-// [2^14, 2^15); a BF16 value has 8 significant bits, so the scaling is exact for all down to 2^-28 of the largest, and what is below loses less
-// than 2^-39 of it. Every 128 k the FP32 result of the instructions is added to FP32 sums with the product of that power of two and the
-// weights' global scale, which is constant there in every scale mode.
+// shared memory in that order. FP16 also holds X: a token's 128 values are divided by the power of four r^2 that brings their largest magnitude
+// to [2^14, 2^16); a BF16 value has 8 significant bits, so the largest stays below FP16's end, the scaling is exact for all down to 2^-28 of
+// the largest, and what is below loses less than 2^-39 of it. Every 128 k the FP32 result d of the instructions is added to FP32 sums with r^2
+// and the weights' global scale g, which is constant there in every scale mode, as (d r) (r g): r^2 g by itself is a subnormal number, of few
+// bits, for tokens below 2^-100, whose results still are normal ones.
 // The outlier channels go through BF16 instructions, 32 of them per step, with the same rows.
 //
 // A CTA takes a 128-row tile, because that is whose scale bytes lie together, 256 k at a time: one tensor copy of 128 bytes of its rows (128-byte
@@ -172,17 +173,17 @@ __device__ __forceinline__ uint4 load_piece(const GemvArgs& a, int64_t m, int i,
   if (!a.keep && k + 8 <= a.K) return *reinterpret_cast<const uint4*>(row + k);
   return code || l16 < 4 ? x8_apart(row, code ? a.keep : a.outl, k, code ? a.K : a.n_out, a.D) : make_uint4(0, 0, 0, 0);
 }
-// Stores them as the instructions read them: [4 words of a lane's 16 codes][token][lane t] 16 bytes, and the power of two that they are to be
-// multiplied by again. Every lane of a warp calls this; `live`: this one's unit exists.
+// Stores them as the instructions read them: [4 words of a lane's 16 codes][token][lane t] 16 bytes, and the power of two r that they are to be
+// multiplied by again, twice. Every lane of a warp calls this; `live`: this one's unit exists.
 __device__ __forceinline__ void store_piece(uint4 w, bool code, bool live, int l16, int m, int Mg, uint8_t* at, float* scale) {
   const uint32_t m2 = amax16x2(amax16x2(w.x, w.y), amax16x2(w.z, w.w));
   uint32_t big = max(m2 & 0x7FFFu, (m2 >> 16) & 0x7FFFu);  // (bit patterns of magnitudes are ordered like them)
 #pragma unroll
   for (int o = 1; o < 16; o <<= 1) big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, o));
   if (!live) return;
-  const uint32_t e = max(big >> 7, 15u);
+  const int e = (int)max(big >> 7, 15u), r = (e - 141) >> 1;  // -63 .. 57
   if (code) {
-    const float to = __uint_as_float((268u - e) << 23);  // 2^(141 - e)
+    const float to = __uint_as_float((uint32_t)(127 - 2 * r) << 23);  // 2^(-2 r)
     const uint32_t wj[4] = {w.x, w.y, w.z, w.w};
     uint32_t h[4];
 #pragma unroll
@@ -192,7 +193,7 @@ __device__ __forceinline__ void store_piece(uint4 w, bool code, bool live, int l
       h[j] = *reinterpret_cast<const uint32_t*>(&q);
     }
     *reinterpret_cast<uint4*>(at + (((l16 & 3) * Mg + m) * 4 + (l16 >> 2)) * 16) = make_uint4(h[0], h[1], h[2], h[3]);
-    if (l16 == 0) *scale = __uint_as_float((e - 14u) << 23);  // 2^(e - 141)
+    if (l16 == 0) *scale = __uint_as_float((uint32_t)(127 + r) << 23);  // 2^r
   } else if (l16 < 4) {
     *reinterpret_cast<uint4*>(at + (m * 4 + l16) * 16) = w;
   }
@@ -414,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, MT > 2 ? 1 : 2) gemv_kernel(const __
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {  // column 2 t + (e & 1): lane (2 t + (e & 1)) & 3 of token 2 n + (t >> 1)
                   const float2 scale = __half22float2(*reinterpret_cast<const __half2*>(&sc[2 * (k0 + k) + (e >> 1)][e & 1]));
-                  acc[k0 + k][n][e] = fmaf(fmaf(d[n][k][1][e], scale.y, d[n][k][0][e] * scale.x), x0 * gv[2 * (k0 + k) + (e >> 1)], acc[k0 + k][n][e]);
+                  acc[k0 + k][n][e] = fmaf(fmaf(d[n][k][1][e], scale.y, d[n][k][0][e] * scale.x) * x0, x0 * gv[2 * (k0 + k) + (e >> 1)], acc[k0 + k][n][e]);
                 }
             }
           }
@@ -440,10 +441,10 @@ __global__ void __launch_bounds__(kThreads, MT > 2 ? 1 : 2) gemv_kernel(const __
             const float x0 = shared_f32(xsc + n * 32), x1 = shared_f32(xsc + n * 32 + 4);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              acc[k][n][0] = fmaf(d[k][n][0], x0 * gv[2 * k], acc[k][n][0]);
-              acc[k][n][1] = fmaf(d[k][n][1], x1 * gv[2 * k], acc[k][n][1]);
-              acc[k][n][2] = fmaf(d[k][n][2], x0 * gv[2 * k + 1], acc[k][n][2]);
-              acc[k][n][3] = fmaf(d[k][n][3], x1 * gv[2 * k + 1], acc[k][n][3]);
+              acc[k][n][0] = fmaf(d[k][n][0] * x0, x0 * gv[2 * k], acc[k][n][0]);
+              acc[k][n][1] = fmaf(d[k][n][1] * x1, x1 * gv[2 * k], acc[k][n][1]);
+              acc[k][n][2] = fmaf(d[k][n][2] * x0, x0 * gv[2 * k + 1], acc[k][n][2]);
+              acc[k][n][3] = fmaf(d[k][n][3] * x1, x1 * gv[2 * k + 1], acc[k][n][3]);
             }
           }
         } else if (!code) {  // 32 outlier channels
