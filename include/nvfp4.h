@@ -456,16 +456,22 @@ nvfp4_status nvfp4_osci_sparse_suppress(float* W, int64_t ldw, int64_t C, int64_
  *            0 .. D-1 is read as NaN.
  *   bias     optional BF16 [N].
  *   Y        [M, N], leading dimension ldy, dtype y_dtype, 16-byte aligned rows. Columns from N on are left as they were.
- *   dev_status optional, see nvfp4_gemm (the waits are for copies of the weights).
+ *   dev_status optional, see nvfp4_gemm (the waits are for copies of the weights and, from three tokens on, of X).
  *   workspace nvfp4_gemv_workspace_bytes(M, D, n_out) bytes, 16-byte aligned (none for one and two tokens; may then be NULL).
  * Products of X and P * S_block are exact, sums are FP32 in an order that M does not change within 1 .. 2, within 3 .. 4 and from 5 on; an element of X below 2^-28 of its token's
  * largest in 128 columns may lose up to 2^-39 of that largest one. Non-finite elements of X give non-finite results of their token.
  * Errors: NULL / ENUM / SHAPE (K + n_out != D, K <= 0) / LIMIT (M > 2097120, D > 2^24, or more than 2^35 pieces of 128 columns of X) / ALIGN / WORKSPACE / ARCH; nothing is launched on an error.
+ *
+ * nvfp4_gemv_ex is the same with a bound of its own for the waits and the test hook of nvfp4_gemm_ex (opts == NULL gives nvfp4_gemv). There are no
+ * variants to choose: ENUM unless opts->variant is AUTO.
  * --------------------------------------------------------------------------------------------------------- */
 size_t nvfp4_gemv_workspace_bytes(int64_t M, int64_t D, int64_t n_out);
 nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, const nvfp4_operand* W, const int32_t* keep_cols,
                         const int32_t* outlier_cols, int64_t n_out, const void* W_out, const void* bias_bf16, void* Y, int32_t y_dtype,
                         int64_t ldy, int32_t* dev_status, void* workspace, size_t ws_bytes, void* stream);
+nvfp4_status nvfp4_gemv_ex(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, const nvfp4_operand* W, const int32_t* keep_cols,
+                           const int32_t* outlier_cols, int64_t n_out, const void* W_out, const void* bias_bf16, void* Y, int32_t y_dtype,
+                           int64_t ldy, int32_t* dev_status, const nvfp4_gemm_opts* opts, void* workspace, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------------------
  * Activation checkpoints in 8 bits: what the steps around the linears keep for backward, in half of BF16's bytes. (The linears themselves

@@ -118,6 +118,8 @@ EXPORTS = {
     "nvfp4_dense_gemm": (c_i32, [ctypes.POINTER(CDenseOperand), ctypes.POINTER(CDenseOperand), c_vp, c_i32, c_i64, c_vp, c_vp]),
     "nvfp4_gemv_workspace_bytes": (c_sz, [c_i64, c_i64, c_i64]),
     "nvfp4_gemv": (c_i32, [c_vp, c_i64, c_i64, c_i64, ctypes.POINTER(COperand), c_vp, c_vp, c_i64, c_vp, c_vp, c_vp, c_i32, c_i64, c_vp, c_vp, c_sz, c_vp]),
+    "nvfp4_gemv_ex": (c_i32, [c_vp, c_i64, c_i64, c_i64, ctypes.POINTER(COperand), c_vp, c_vp, c_i64, c_vp, c_vp, c_vp, c_i32, c_i64, c_vp,
+                              ctypes.POINTER(CGemmOpts), c_vp, c_sz, c_vp]),
     "nvfp4_ckpt8_ld": (c_i64, [c_i64]),
     "nvfp4_ckpt8_pack": (c_i32, [c_vp, c_i32, c_i64, c_i64, c_i64, ctypes.POINTER(CCkpt8), c_vp]),
     "nvfp4_ckpt8_unpack": (c_i32, [ctypes.POINTER(CCkpt8), c_vp, c_i32, c_i64, c_vp]),
@@ -854,11 +856,24 @@ SAVE_NOTHING, SAVE_INPUT, SAVE_CKPT8 = 0, 1, 2  # what a forward call keeps for 
 
 
 def nvfp4_gemv(X: torch.Tensor, W: Operand, c_dtype: int = DT_BF16, bias: torch.Tensor | None = None, index: tuple | None = None,
-               W_out: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+               W_out: torch.Tensor | None = None, out: torch.Tensor | None = None, dev_status: torch.Tensor | None = None) -> torch.Tensor:
     """X [tokens, D] times quantized weights, for few tokens: X stays BF16. With outlier channels, `index` starts with (outlier columns, kept
-    columns) and W_out holds their weights (Saved.W_out)."""
+    columns) and W_out holds their weights (Saved.W_out). dev_status: int32 on X's device, set to ERR_TIMEOUT where a wait ran out."""
     outl, keep = (None, None) if index is None else (index[0], index[1])
-    return _node.gemv(X, W.codes, W.sf, W.gscale, W.R, W.K, W.gs_mode, W.sf_layout, c_dtype, bias, outl, keep, W_out, out)
+    return _node.gemv(X, W.codes, W.sf, W.gscale, W.R, W.K, W.gs_mode, W.sf_layout, c_dtype, bias, outl, keep, W_out, out, dev_status)
+
+
+def nvfp4_gemv_ex(X: torch.Tensor, W: Operand, c_dtype: int = DT_BF16, dev_status: torch.Tensor | None = None, wait_limit_cycles: int = 0,
+                  starve_first_stage: bool = False) -> torch.Tensor:
+    """nvfp4_gemv (without outlier channels) with an explicit wait bound and the test hook of the bounded waits."""
+    assert X.dtype == torch.bfloat16 and X.dim() == 2 and X.stride(1) == 1
+    M, D = X.shape
+    out = _matrix(M, W.R, c_dtype, X.device)
+    ws = _workspace(_lib.nvfp4_gemv_workspace_bytes(M, D, 0), X.device)
+    cw, opts = W.c(), CGemmOpts(GEMM_AUTO, int(starve_first_stage), wait_limit_cycles)
+    _check(_lib.nvfp4_gemv_ex(_ptr(X), X.stride(0), M, D, ctypes.byref(cw), None, None, 0, None, None, _ptr(out), c_dtype, out.stride(0), _ptr(dev_status),
+                              ctypes.byref(opts), _ptr(ws), ws.numel(), _stream_ptr()), "nvfp4_gemv_ex")
+    return out
 
 
 @dataclass(slots=True)

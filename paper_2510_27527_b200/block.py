@@ -71,9 +71,10 @@ class _SwigluFn(torch.autograd.Function):
         return *B.nvfp4_swiglu_bwd(_rows(_bf16(dh), D, "swiglu"), s), None
 
 
-def _gemv(x, codes, scales, global_scales, outlier_cols, keep_cols, outlier_weight, bias, N, K, gs_mode):
+def _gemv(x, codes, scales, global_scales, outlier_cols, keep_cols, outlier_weight, bias, form):
+    N, K, gs_mode, dev_status = form
     W = B.Operand(codes, scales, global_scales, N, K, gs_mode, B.SF_TILED128x4)
-    return B.nvfp4_gemv(x, W, B.DT_BF16, bias, None if outlier_cols is None else (outlier_cols, keep_cols), outlier_weight)
+    return B.nvfp4_gemv(x, W, B.DT_BF16, bias, None if outlier_cols is None else (outlier_cols, keep_cols), outlier_weight, None, dev_status)
 
 
 class _FrozenFn(torch.autograd.Function):
@@ -132,15 +133,15 @@ class NVFP4LayerNorm(torch.nn.Module):
 
 class NVFP4FrozenLinear(torch.nn.Module):
     """y = x W-hat^T (+ bias) with the weights as NVFP4Linear's forward quantizes them (OutControl's outlier channels in high precision) and x in
-    BF16: for answering, a few tokens at a time. No gradients."""
+    BF16: for answering, a few tokens at a time. No gradients. A wait that runs out is reported in the layer's cfg.dev_status, as in training."""
 
     def __init__(self, layer: NVFP4Linear):
         super().__init__()
         self.in_features, self.out_features = layer.in_features, layer.out_features
         if not layer.weight.is_cuda or layer.weight.dtype != torch.bfloat16:
             raise RuntimeError(f"NVFP4FrozenLinear: weights of {layer.weight.dtype} on {layer.weight.device}, not BF16 on a CUDA device")
-        cfg = dataclasses.replace(layer.cfg, dev_status=None, y_dtype=B.DT_BF16)
-        self.gs_mode, self.n_out = cfg.gs_mode, cfg.n_out
+        cfg = dataclasses.replace(layer.cfg, y_dtype=B.DT_BF16)
+        self.gs_mode, self.n_out, self.dev_status = cfg.gs_mode, cfg.n_out, cfg.dev_status
         with torch.no_grad(), torch.cuda.device(layer.weight.device):  # the call that quantizes the weights in training, on one token
             _, saved = B.nvfp4_linear_fwd(torch.ones((1, self.in_features), dtype=torch.bfloat16, device=layer.weight.device), layer.weight.detach(), cfg)
             index = saved.index if self.n_out else (None, None)
@@ -160,8 +161,8 @@ class NVFP4FrozenLinear(torch.nn.Module):
         if _wants_grad(x):
             raise RuntimeError("NVFP4FrozenLinear has no gradient: use it under torch.no_grad()")
         rows = _rows(_bf16(x), self.in_features, "NVFP4FrozenLinear")
-        y = _frozen(rows, self.codes, self.scales, self.global_scales, self.outlier_cols, self.keep_cols, self.outlier_weight, self.bias, self.out_features,
-                    self.in_features - self.n_out, self.gs_mode)
+        y = _frozen(rows, self.codes, self.scales, self.global_scales, self.outlier_cols, self.keep_cols, self.outlier_weight, self.bias,
+                    (self.out_features, self.in_features - self.n_out, self.gs_mode, self.dev_status))
         return y if x.dim() == 2 else y.reshape(*x.shape[:-1], self.out_features)
 
 

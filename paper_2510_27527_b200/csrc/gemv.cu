@@ -72,6 +72,8 @@ struct GemvArgs {
   uint8_t* staged;       // X staged in memory: [32 tokens][pair] pair_bytes
   int wide;              // tokens that an instruction's width is rounded to, of the kernel that reads it
   int32_t* dev_status;
+  long long wait_limit;  // bound of every wait, in clock cycles
+  int starve;            // test hook of the waits: the first stage never completes
 };
 
 __device__ __forceinline__ uint4 shared16(uint32_t at) {
@@ -272,9 +274,9 @@ __global__ void __launch_bounds__(kThreads, MT > 2 ? 1 : 2) gemv_kernel(const __
         pdl_wait();
         for (int f = 0; f < STAGES; ++f) bring_x(p_begin + f, f);
       }
-      if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&empty[i]), phase, &abort_flag, a.dev_status, DEFAULT_WAIT_LIMIT_CYCLES))) break;
+      if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&empty[i]), phase, &abort_flag, a.dev_status, a.wait_limit))) break;
       if (p < a.n_code_pairs) {
-        mbar_expect_tx(bar, kStageBytes + x_bytes, leader);
+        mbar_expect_tx(bar, kStageBytes + x_bytes + (a.starve && p == p_begin ? 16 : 0), leader);
         tma_load_2d(to, &codes_map, p * 128, (int32_t)(rb * kRows), bar, leader);
         bulk_load(to + kCodeBytes, a.sf + ((int64_t)rb * (nbp >> 2) + (int64_t)p * 4) * 512, kScaleBytes, bar, leader);
       } else {
@@ -346,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, MT > 2 ? 1 : 2) gemv_kernel(const __
         consumer_barrier();
 #pragma unroll 1
       for (int p = q0; p < q0 + n_seg / 2; ++p) {
-        if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&full[s]), phase, &abort_flag, a.dev_status, DEFAULT_WAIT_LIMIT_CYCLES))) break;
+        if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&full[s]), phase, &abort_flag, a.dev_status, a.wait_limit))) break;
         const uint32_t at = ring + s * stage_bytes;
         const int i = 2 * p + half;  // this warp's piece
         const uint32_t xp = SEP ? xs_at + (p - q0) * 512 * Mg : at + kStageBytes;  // this pair of X
@@ -525,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, MT > 2 ? 1 : 2) gemv_kernel(const __
   if (warp == kConsumers / 32 && *(volatile int*)&abort_flag) {  // a wait ran out: the copies under way get the same time to land before the CTA ends
     for (int f = max(0, filled - STAGES); f < filled; ++f) {
       const long long t0 = clock64();
-      while (!mbar_test(smem_u32(&full[f % STAGES]), (uint32_t)(f / STAGES) & 1u) && clock64() - t0 < DEFAULT_WAIT_LIMIT_CYCLES) {
+      while (!mbar_test(smem_u32(&full[f % STAGES]), (uint32_t)(f / STAGES) & 1u) && clock64() - t0 < a.wait_limit) {
       }
     }
   }
@@ -576,7 +578,14 @@ size_t nvfp4_gemv_workspace_bytes(int64_t M, int64_t D, int64_t n_out) {
 nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, const nvfp4_operand* W, const int32_t* keep_cols, const int32_t* outlier_cols,
                         int64_t n_out, const void* W_out, const void* bias_bf16, void* Y, int32_t y_dtype, int64_t ldy, int32_t* dev_status, void* workspace, size_t ws_bytes,
                         void* stream) {
+  return nvfp4_gemv_ex(X_bf16, ldx, M, D, W, keep_cols, outlier_cols, n_out, W_out, bias_bf16, Y, y_dtype, ldy, dev_status, nullptr, workspace, ws_bytes, stream);
+}
+
+nvfp4_status nvfp4_gemv_ex(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, const nvfp4_operand* W, const int32_t* keep_cols, const int32_t* outlier_cols,
+                           int64_t n_out, const void* W_out, const void* bias_bf16, void* Y, int32_t y_dtype, int64_t ldy, int32_t* dev_status, const nvfp4_gemm_opts* opts,
+                           void* workspace, size_t ws_bytes, void* stream) {
   if (!W) return NVFP4_ERR_NULL;
+  if (opts && (opts->variant != NVFP4_GEMM_AUTO || opts->wait_limit_cycles < 0)) return NVFP4_ERR_ENUM;
   if (W->gs_mode < 0 || W->gs_mode > 2 || W->sf_layout != NVFP4_SF_TILED128x4 || y_dtype < 0 || y_dtype > 1) return NVFP4_ERR_ENUM;
   if (M < 0 || D <= 0 || n_out < 0 || W->R < 0 || W->K <= 0 || W->K + n_out != D) return NVFP4_ERR_SHAPE;
   if (D > ((int64_t)1 << 24) || W->R > ((int64_t)1 << 31) || M > 65535ll * kMaxTokens) return NVFP4_ERR_LIMIT;
@@ -614,6 +623,8 @@ nvfp4_status nvfp4_gemv(const void* X_bf16, int64_t ldx, int64_t M, int64_t D, c
   a.n_code_pairs = (int)n_code_pairs;
   a.n_pairs = (int)n_pairs;
   a.dev_status = dev_status;
+  a.wait_limit = opts && opts->wait_limit_cycles > 0 ? opts->wait_limit_cycles : DEFAULT_WAIT_LIMIT_CYCLES;
+  a.starve = opts && opts->starve_first_stage;
   CUtensorMap codes{}, outliers{};
   if (!encode_codes_map(&codes, W->codes, W->R, nvfp4_padded_k(W->K)) || (n_out > 0 && !encode_outliers_map(&outliers, W_out, W->R, a.Kh))) return NVFP4_ERR_CUDA;
   // CTAs along k: as many as leave every CTA a pair and give an SM two of them

@@ -104,11 +104,11 @@ struct Guard {
 };
 
 // ---- the calls -----------------------------------------------------------------------------------------------------------------------
-// gemv(X, codes, sf, gscale, R, K, gs_mode, sf_layout, dtype code, bias, outlier columns, kept columns, W_out, out)
+// gemv(X, codes, sf, gscale, R, K, gs_mode, sf_layout, dtype code, bias, outlier columns, kept columns, W_out, out, dev_status)
 PyObject* gemv(PyObject*, Args a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   const char* where = "nvfp4_gemv";
-  count(n, 14, where);
+  count(n, 15, where);
   const at::Tensor& X = tensor(a[0], where, "X");
   const c10::Device dev = X.device();
   const int64_t ldx = rows_of(X, where, "X", at::kBFloat16, -1, -1, dev), M = X.size(0), D = X.size(1);
@@ -139,12 +139,13 @@ PyObject* gemv(PyObject*, Args a, Py_ssize_t n) {
       W_out = w.data_ptr();
     }
   }
+  int32_t* status = given(a[14]) ? static_cast<int32_t*>(bytes(tensor(a[14], where, "dev_status"), where, "dev_status", 4, dev, at::kInt)) : nullptr;
   TORCH_CHECK(W.R >= 0, where, ": ", W.R, " weight rows");
   at::Tensor Y = given(a[13]) ? tensor(a[13], where, "out") : matrix(M, W.R, X.options().dtype(type));
   const int64_t ldy = rows_of(Y, where, "out", type, M, W.R, dev);
   const size_t need = nvfp4_gemv_workspace_bytes(M, D, n_out);
   const at::Tensor ws = need ? at::empty({(int64_t)need}, X.options().dtype(at::kByte)) : at::Tensor();
-  check(nvfp4_gemv(X.data_ptr(), ldx, M, D, &W, keep, outl, n_out, W_out, bias, Y.data_ptr(), code_of(type), ldy, nullptr, need ? ws.data_ptr() : nullptr, need,
+  check(nvfp4_gemv(X.data_ptr(), ldx, M, D, &W, keep, outl, n_out, W_out, bias, Y.data_ptr(), code_of(type), ldy, status, need ? ws.data_ptr() : nullptr, need,
                    current_stream()), where);
   return wrap(Y);
   END_HANDLE_TH_ERRORS
