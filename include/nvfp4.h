@@ -499,7 +499,9 @@ nvfp4_status nvfp4_ckpt8_unpack(const nvfp4_ckpt8* in, void* X, int32_t x_dtype,
 
 /* ---------------------------------------------------------------------------------------------------------
  * SwiGLU, the input of the down projection: h = g s u with s = 1 / (1 + exp(-g)); dg = dh u s (1 + g (1 - s)), du = dh g s.
- * All matrices BF16 [T, D] with their own leading dimensions and 16-byte aligned rows; FP32 arithmetic, one rounding per result.
+ * All matrices BF16 [T, D] with their own leading dimensions and 16-byte aligned rows. The arithmetic is FP32 and each result is rounded to BF16
+ * once: s is off by (6 + 1.2 |g|) 2^-23 of itself at most, every product and sum by 2^-24 (1 - s of 1). s is 0 for g < -88.72, where it is below
+ * 2^-128.
  *   fwd: g8 and u8 both NULL, or both checkpoints [T, D] to be filled with G and U beside H. H may be G or U.
  *   bwd: with g8 and u8 the values are the checkpoints' (G and U are not looked at), else G's and U's. dG and dU may be dH, G or U, but not
  *        one another.

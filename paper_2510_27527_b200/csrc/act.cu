@@ -4,7 +4,7 @@
 //   nvfp4_swiglu_bwd             dg = dh u s (1 + g (1 - s)), du = dh g s, with g and u from their BF16 values or their checkpoints
 // All of them stream: a thread takes eight neighbouring elements of a row, so that every load and store of a warp is contiguous.
 // Measured (us, inputs from HBM; in brackets the share of the copy bandwidth): 16384 x 8192 BF16 packed 59.1 (1.06), unpacked 62.7 (1.00); SwiGLU
-// 16384 x 2816 forward 40.9 (1.04), with checkpoints 59.8 (0.96), backward 68.7 (1.03), from checkpoints 58.1 (0.98). Memory bounds them.
+// 16384 x 2816 forward 40.8 (1.04), with checkpoints 60.0 (0.96), backward 68.5 (1.03), from checkpoints 57.7 (0.99). Memory bounds them.
 #include "../../include/nvfp4.h"
 
 #include <type_traits>
@@ -23,7 +23,7 @@ __device__ __forceinline__ int64_t quotient(int64_t n, int64_t d, int64_t total)
 
 // FLAT, of every kernel here: matrices without gaps (leading dimensions that are D, and D a multiple of the group where there are checkpoints),
 // whose pieces of eight need no row and column: fewer instructions for what is bound by them and by memory alike (SwiGLU forward with
-// checkpoints, 16384 x 2816: 66.6 us with rows and columns, 59.8 without).
+// checkpoints, 16384 x 2816: 66.6 us with rows and columns, 60.0 without).
 //
 // NB pieces of eight elements a thread, one CTA's next to one another: one piece's loads of all threads of an SM (32 KB from BF16, 16 KB of
 // codes) are fewer than memory needs in flight.
@@ -90,12 +90,18 @@ __global__ void __launch_bounds__(256) ckpt8_unpack_kernel(ActSrc x, int64_t R, 
   }
 }
 
-// 1 / (1 + exp(-g)): 1 at +inf, 0 at -inf
-__device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
-
+// 1 / (1 + exp(-g)), exp(-g) = 2^(-g log2 e): 1 at +inf, 0 at -inf. The quotient of a quarter of the denominator, a quarter of it: in range for
+// every finite one, where the fast division gives 0 for those above 2^126, whose quotients are subnormal numbers that make normal products with a
+// large u (g = -88, u = 2^20: 2^-101). Below g = -88.72 the power is infinite and the result 0; a power below 2^-126 is nothing beside 1.
+__device__ __forceinline__ float power2(float t) {
+  float p;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(t));
+  return p;
+}
 __device__ __forceinline__ f32x2 sigmoid2(f32x2 g) {
-  const float2 v = values_of(g);
-  return pair_of(sigmoid(v.x), sigmoid(v.y));
+  const float2 t = values_of(mul2(g, pair_of(-1.44269504f)));
+  const float2 y = values_of(fma2(pair_of(power2(t.x), power2(t.y)), pair_of(0.25f), pair_of(0.25f)));
+  return mul2(pair_of(__fdividef(1.0f, y.x), __fdividef(1.0f, y.y)), pair_of(0.25f));
 }
 
 struct CkptOut {
