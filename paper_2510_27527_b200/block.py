@@ -131,7 +131,19 @@ class NVFP4LayerNorm(torch.nn.Module):
         return y if x.dim() == 2 else y.reshape(x.shape)
 
 
-class NVFP4FrozenLinear(torch.nn.Module):
+class _Frozen(torch.nn.Module):
+    """A module whose buffers keep the types they were frozen in: a model's change of type is not for them, one of device is."""
+
+    def _apply(self, fn, recurse=True):
+        before = {n: b for n, b in self._buffers.items() if b is not None}
+        super()._apply(fn, recurse)
+        for n, b in before.items():
+            if self._buffers[n].dtype != b.dtype:
+                self._buffers[n] = b.to(self._buffers[n].device)
+        return self
+
+
+class NVFP4FrozenLinear(_Frozen):
     """y = x W-hat^T (+ bias) with the weights as NVFP4Linear's forward quantizes them (OutControl's outlier channels in high precision) and x in
     BF16: for answering, a few tokens at a time. No gradients. A wait that runs out is reported in the layer's cfg.dev_status, as in training."""
 
@@ -148,14 +160,6 @@ class NVFP4FrozenLinear(torch.nn.Module):
             for name, t in (("codes", saved.qw.codes), ("scales", saved.qw.sf), ("global_scales", saved.qw.gscale), ("outlier_cols", index[0]), ("keep_cols", index[1]),
                             ("outlier_weight", saved.W_out), ("bias", None if layer.bias is None else layer.bias.detach())):
                 self.register_buffer(name, None if t is None else t.clone())
-
-    def _apply(self, fn, recurse=True):  # (a model's change of type is not for the operand's arrays, which have one each; one of device is)
-        before = {n: b for n, b in self._buffers.items() if b is not None}
-        super()._apply(fn, recurse)
-        for n, b in before.items():
-            if self._buffers[n].dtype != b.dtype:
-                self._buffers[n] = b.to(self._buffers[n].device)
-        return self
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         if _wants_grad(x):
@@ -190,7 +194,7 @@ class NVFP4MLP(torch.nn.Module):
         return NVFP4FrozenMLP(self)
 
 
-class NVFP4FrozenMLP(torch.nn.Module):
+class NVFP4FrozenMLP(_Frozen):
     """NVFP4MLP for a few tokens at a time: its weights quantized once, activations in BF16. No gradients."""
 
     def __init__(self, mlp: NVFP4MLP):

@@ -110,3 +110,17 @@ def test_a_frozen_layers_parameters_have_no_gradient():
     y = torch.func.functional_call(f, {"bias": bias}, (x,))
     with pytest.raises(RuntimeError, match="no gradient"):
         y.sum().backward()
+
+
+@pytest.mark.parametrize("norm_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("change", ["half", "double", "float", "bfloat16"])
+def test_a_frozen_models_change_of_type_changes_no_answer(change, norm_dtype):
+    from paper_2510_27527_b200.block import NVFP4MLP
+
+    mlp, x = NVFP4MLP(64, 128, norm_dtype=norm_dtype), mk(3, 64)
+    with torch.no_grad():
+        mlp.norm.weight.add_(torch.randn(64, device="cuda") * 0.1)
+        f = mlp.frozen()
+        want = f(x)
+        assert torch.equal(getattr(f, change)()(x), want) and f.norm_weight.dtype == norm_dtype
+        assert torch.equal(torch.nn.Sequential(f).to(torch.float16)(x), want)
