@@ -165,12 +165,22 @@ def measure_lib():
     return _measure_lib
 
 
-try:  # (linked with the library above)
+class _NoNode:
+    """In the place of the compiled module where it cannot be loaded: the calls that it makes are refused, those through ctypes work."""
+
+    def __init__(self, error: ImportError):
+        self.error = error
+
+    def __getattr__(self, name):
+        raise ImportError(f"{self.error}: build it with `python -m paper_2510_27527_b200.build`") from self.error
+
+
+try:  # (linked with the library above; made for one torch and one Python)
     from . import _node
     if getattr(_node, "built_for", None) != node_tag():  # (it may load all the same)
         raise ImportError(f"{_node.__file__} is not for {node_tag()}")
 except ImportError as e:
-    raise ImportError(f"{e}: build it with `python -m paper_2510_27527_b200.build`") from e
+    _node = _NoNode(e)
 
 
 class Nvfp4Error(RuntimeError):

@@ -16,6 +16,8 @@ from torch.autograd import forward_ad
 from . import binding as B
 from .binding import _node
 
+_node.linear  # (an ImportError here where the compiled module is missing, not at the first call)
+
 
 _MASK64 = (1 << 64) - 1
 
