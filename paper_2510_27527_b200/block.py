@@ -49,7 +49,7 @@ class _LayerNormFn(torch.autograd.Function):
     def backward(ctx, dy):
         gamma, stats, x = ctx.saved_tensors
         T, D, x_dtype, has_beta, checkpoint = ctx.saved
-        kept = dict(x8=B.Ckpt8(x, T, D)) if checkpoint else dict(X=x)
+        kept = dict(x8=B.Ckpt8(x, T, D)) if checkpoint else dict(X=_rows(x, D, "NVFP4LayerNorm"))  # (a hook may have given it other strides)
         dx, dgamma, dbeta = B.nvfp4_layernorm_bwd(_rows(_bf16(dy), D, "NVFP4LayerNorm"), B.LayerNormSaved(T, D, x_dtype, stats, gamma, has_beta, **kept))
         return dx, dgamma, dbeta, None, None
 
@@ -67,7 +67,7 @@ class _SwigluFn(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dh):
         (a, b), (T, D, checkpoint) = ctx.saved_tensors, ctx.saved
-        s = B.SwigluSaved(T, D, g8=B.Ckpt8(a, T, D), u8=B.Ckpt8(b, T, D)) if checkpoint else B.SwigluSaved(T, D, a, b)
+        s = B.SwigluSaved(T, D, g8=B.Ckpt8(a, T, D), u8=B.Ckpt8(b, T, D)) if checkpoint else B.SwigluSaved(T, D, _rows(a, D, "swiglu"), _rows(b, D, "swiglu"))
         return *B.nvfp4_swiglu_bwd(_rows(_bf16(dh), D, "swiglu"), s), None
 
 

@@ -124,3 +124,21 @@ def test_a_frozen_models_change_of_type_changes_no_answer(change, norm_dtype):
         want = f(x)
         assert torch.equal(getattr(f, change)()(x), want) and f.norm_weight.dtype == norm_dtype
         assert torch.equal(torch.nn.Sequential(f).to(torch.float16)(x), want)
+
+
+@pytest.mark.parametrize("checkpoint", [False, True])
+@pytest.mark.parametrize("width", [64, 33])  # (rows of 33 are padded, their copies are not)
+def test_inputs_kept_elsewhere(width, checkpoint):
+    """torch.autograd.graph.save_on_cpu brings back contiguous copies."""
+    from paper_2510_27527_b200.block import NVFP4LayerNorm, swiglu
+
+    ln, x, dy = NVFP4LayerNorm(width, checkpoint=checkpoint), mk(6, width).requires_grad_(), mk(6, width)
+
+    def step():
+        y = swiglu(ln(x), x * 1, checkpoint)
+        return y, lambda: torch.autograd.grad(y, (x, ln.weight, ln.bias), dy)
+
+    want = step()[1]()
+    with torch.autograd.graph.save_on_cpu():
+        y, grads = step()
+    assert all(torch.equal(p, q) for p, q in zip(grads(), want))
