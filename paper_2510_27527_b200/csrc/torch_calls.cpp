@@ -10,6 +10,8 @@
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
+#include <pybind11/pybind11.h>
+
 using nvfp4_torch::matrix;
 using nvfp4_torch::raise_status;
 using nvfp4_torch::up;
@@ -92,7 +94,14 @@ PyObject* tuple_of(const T&... t) {
   return r;
 }
 void* current_stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
-void check(nvfp4_status s, const char* where) {
+// The library call, without Python's lock: a launch waits where the device's queue is full.
+template <typename F>
+void enqueue(const char* where, F&& call) {
+  nvfp4_status s;
+  {
+    pybind11::gil_scoped_release no_gil;
+    s = call();
+  }
   if (s != NVFP4_OK) raise_status(s, where);
 }
 // The tensors' device is the current one while a call lasts. (A device of another kind is refused by the checks.)
@@ -145,8 +154,8 @@ PyObject* gemv(PyObject*, Args a, Py_ssize_t n) {
   const int64_t ldy = rows_of(Y, where, "out", type, M, W.R, dev);
   const size_t need = nvfp4_gemv_workspace_bytes(M, D, n_out);
   const at::Tensor ws = need ? at::empty({(int64_t)need}, X.options().dtype(at::kByte)) : at::Tensor();
-  check(nvfp4_gemv(X.data_ptr(), ldx, M, D, &W, keep, outl, n_out, W_out, bias, Y.data_ptr(), code_of(type), ldy, status, need ? ws.data_ptr() : nullptr, need,
-                   current_stream()), where);
+  enqueue(where, [&] { return nvfp4_gemv(X.data_ptr(), ldx, M, D, &W, keep, outl, n_out, W_out, bias, Y.data_ptr(), code_of(type), ldy, status, need ? ws.data_ptr() : nullptr, need,
+                   current_stream()); });
   return wrap(Y);
   END_HANDLE_TH_ERRORS
 }
@@ -162,7 +171,7 @@ PyObject* ckpt8_pack(PyObject*, Args a, Py_ssize_t n) {
   const Guard guard(dev);
   at::Tensor buf = given(a[1]) ? tensor(a[1], where, "the checkpoint") : new_ckpt8(R, K, X.options());
   const nvfp4_ckpt8 c = ckpt8(buf, where, R, K, dev);
-  check(nvfp4_ckpt8_pack(X.data_ptr(), code_of(X.scalar_type()), ldx, R, K, &c, current_stream()), where);
+  enqueue(where, [&] { return nvfp4_ckpt8_pack(X.data_ptr(), code_of(X.scalar_type()), ldx, R, K, &c, current_stream()); });
   return wrap(buf);
   END_HANDLE_TH_ERRORS
 }
@@ -180,7 +189,7 @@ PyObject* ckpt8_unpack(PyObject*, Args a, Py_ssize_t n) {
   const Guard guard(dev);
   at::Tensor X = given(a[4]) ? tensor(a[4], where, "out") : matrix(R, K, buf.options().dtype(type));
   const int64_t ld = rows_of(X, where, "out", type, R, K, dev);
-  check(nvfp4_ckpt8_unpack(&c, X.data_ptr(), code_of(type), ld, current_stream()), where);
+  enqueue(where, [&] { return nvfp4_ckpt8_unpack(&c, X.data_ptr(), code_of(type), ld, current_stream()); });
   return wrap(X);
   END_HANDLE_TH_ERRORS
 }
@@ -207,7 +216,7 @@ PyObject* swiglu_fwd(PyObject*, Args a, Py_ssize_t n) {
     cg = ckpt8(g8 = new_ckpt8(T, D, G.options()), where, T, D, dev);
     cu = ckpt8(u8 = new_ckpt8(T, D, G.options()), where, T, D, dev);
   }
-  check(nvfp4_swiglu_fwd(G.data_ptr(), ldg, U.data_ptr(), ldu, T, D, H.data_ptr(), ldh, save == kCkpt8 ? &cg : nullptr, save == kCkpt8 ? &cu : nullptr, current_stream()), where);
+  enqueue(where, [&] { return nvfp4_swiglu_fwd(G.data_ptr(), ldg, U.data_ptr(), ldu, T, D, H.data_ptr(), ldh, save == kCkpt8 ? &cg : nullptr, save == kCkpt8 ? &cu : nullptr, current_stream()); });
   return tuple_of(H, g8, u8);
   END_HANDLE_TH_ERRORS
 }
@@ -237,7 +246,7 @@ PyObject* swiglu_bwd(PyObject*, Args a, Py_ssize_t n) {
   }
   at::Tensor dG = given(a[7]) ? tensor(a[7], where, "dG") : matrix(T, D, dH.options()), dU = given(a[8]) ? tensor(a[8], where, "dU") : matrix(T, D, dH.options());
   const int64_t lddg = rows_of(dG, where, "dG", at::kBFloat16, T, D, dev), lddu = rows_of(dU, where, "dU", at::kBFloat16, T, D, dev);
-  check(nvfp4_swiglu_bwd(dH.data_ptr(), lddh, G, ldg, U, ldu, packed ? &cg : nullptr, packed ? &cu : nullptr, T, D, dG.data_ptr(), lddg, dU.data_ptr(), lddu, current_stream()), where);
+  enqueue(where, [&] { return nvfp4_swiglu_bwd(dH.data_ptr(), lddh, G, ldg, U, ldu, packed ? &cg : nullptr, packed ? &cu : nullptr, T, D, dG.data_ptr(), lddg, dU.data_ptr(), lddu, current_stream()); });
   return tuple_of(dG, dU);
   END_HANDLE_TH_ERRORS
 }
@@ -263,8 +272,8 @@ PyObject* layernorm_fwd(PyObject*, Args a, Py_ssize_t n) {
   if (save != kNothing) stats = at::empty({T, 2}, X.options().dtype(at::kFloat));
   nvfp4_ckpt8 c;
   if (save == kCkpt8) c = ckpt8(x8 = new_ckpt8(T, D, X.options()), where, T, D, dev);
-  check(nvfp4_layernorm_fwd(X.data_ptr(), code_of(X.scalar_type()), ldx, T, D, pg, pb, code_of(type), (float)eps, Y.data_ptr(), ldy,
-                            stats.defined() ? static_cast<float*>(stats.data_ptr()) : nullptr, save == kCkpt8 ? &c : nullptr, current_stream()), where);
+  enqueue(where, [&] { return nvfp4_layernorm_fwd(X.data_ptr(), code_of(X.scalar_type()), ldx, T, D, pg, pb, code_of(type), (float)eps, Y.data_ptr(), ldy,
+                            stats.defined() ? static_cast<float*>(stats.data_ptr()) : nullptr, save == kCkpt8 ? &c : nullptr, current_stream()); });
   return tuple_of(Y, stats, x8);
   END_HANDLE_TH_ERRORS
 }
@@ -303,8 +312,8 @@ PyObject* layernorm_bwd(PyObject*, Args a, Py_ssize_t n) {
   const int64_t need = (int64_t)nvfp4_layernorm_bwd_workspace_bytes(T, D);
   const at::Tensor ws = given(a[11]) ? tensor(a[11], where, "the workspace") : at::empty({need}, dY.options().dtype(at::kByte));
   void* pw = bytes(ws, where, "the workspace", 0, dev);
-  check(nvfp4_layernorm_bwd(dY.data_ptr(), lddy, X, code_of(x_type), ldx, packed ? &c : nullptr, T, D, pg, code_of(p_type), static_cast<const float*>(stats.data_ptr()),
-                            dX.data_ptr(), lddx, dgamma.data_ptr(), beta ? dbeta.data_ptr() : nullptr, code_of(d_type), pw, ws.nbytes(), current_stream()), where);
+  enqueue(where, [&] { return nvfp4_layernorm_bwd(dY.data_ptr(), lddy, X, code_of(x_type), ldx, packed ? &c : nullptr, T, D, pg, code_of(p_type), static_cast<const float*>(stats.data_ptr()),
+                            dX.data_ptr(), lddx, dgamma.data_ptr(), beta ? dbeta.data_ptr() : nullptr, code_of(d_type), pw, ws.nbytes(), current_stream()); });
   return tuple_of(dX, dgamma, dbeta);
   END_HANDLE_TH_ERRORS
 }
