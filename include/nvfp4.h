@@ -455,7 +455,8 @@ nvfp4_status nvfp4_osci_sparse_suppress(float* W, int64_t ldw, int64_t C, int64_
  *            16-byte aligned, as in nvfp4_saved (its columns from n_out on are multiplied by zero: finite). A column outside
  *            0 .. D-1 is read as NaN.
  *   bias     optional BF16 [N].
- *   Y        [M, N], leading dimension ldy, dtype y_dtype, 16-byte aligned rows. Columns from N on are left as they were.
+ *   Y        [M, N], leading dimension ldy, dtype y_dtype, 16-byte aligned rows. Columns from N on are left as they were. Not in X's memory: all
+ *            of a token is read while parts of its result are written.
  *   dev_status optional, see nvfp4_gemm (the waits are for copies of the weights and, from three tokens on, of X).
  *   workspace nvfp4_gemv_workspace_bytes(M, D, n_out) bytes, 16-byte aligned (none for one and two tokens; may then be NULL).
  * Products of X and P * S_block are exact, sums are FP32 in an order that M does not change within 1 .. 2, within 3 .. 4 and from 5 on; an element of X below 2^-28 of its token's
@@ -502,9 +503,9 @@ nvfp4_status nvfp4_ckpt8_unpack(const nvfp4_ckpt8* in, void* X, int32_t x_dtype,
  * All matrices BF16 [T, D] with their own leading dimensions and 16-byte aligned rows. The arithmetic is FP32 and each result is rounded to BF16
  * once: s is off by (6 + 1.2 |g|) 2^-23 of itself at most, every product and sum by 2^-24 (1 - s of 1). s is 0 for g < -88.72, where it is below
  * 2^-128.
- *   fwd: g8 and u8 both NULL, or both checkpoints [T, D] to be filled with G and U beside H. H may be G or U.
- *   bwd: with g8 and u8 the values are the checkpoints' (G and U are not looked at), else G's and U's. dG and dU may be dH, G or U, but not
- *        one another.
+ *   fwd: g8 and u8 both NULL, or both checkpoints [T, D] to be filled with G and U beside H. H may be G or U (with its leading dimension).
+ *   bwd: with g8 and u8 the values are the checkpoints' (G and U are not looked at), else G's and U's. dG and dU may be dH, G or U (with
+ *        their leading dimensions), but not one another.
  * Errors as for the checkpoints (SHAPE also where only one of g8, u8 is given).
  * --------------------------------------------------------------------------------------------------------- */
 nvfp4_status nvfp4_swiglu_fwd(const void* G, int64_t ldg, const void* U, int64_t ldu, int64_t T, int64_t D, void* H, int64_t ldh,
@@ -522,7 +523,7 @@ nvfp4_status nvfp4_swiglu_bwd(const void* dH, int64_t lddh, const void* G, int64
  *          those of X).
  *   dgamma, dbeta (NULL: not wanted)  dparam_dtype [D], written also for T = 0. Sums are FP32 in a fixed order.
  *   workspace (backward): nvfp4_layernorm_bwd_workspace_bytes(T, D) bytes, 16-byte aligned.
- * dX may be dY or X where their types are the same. Rows and columns beyond [T, D] are left as they were.
+ * dX may be dY or X, and Y of forward may be X, where their types and leading dimensions are the same. Rows and columns beyond [T, D] are left as they were.
  * Errors: NULL / ENUM / SHAPE (T < 0, D <= 0, eps < 0 or NaN, a checkpoint of another shape) / LIMIT / ALIGN / WORKSPACE / ARCH.
  * --------------------------------------------------------------------------------------------------------- */
 nvfp4_status nvfp4_layernorm_fwd(const void* X, int32_t x_dtype, int64_t ldx, int64_t T, int64_t D, const void* gamma, const void* beta,

@@ -7,6 +7,7 @@
 // or a SwiGLU of a few tokens took 12.5 to 13.3 us from Python, this way 4.5 to 5.5.
 #include "torch_common.h"
 
+#include <ATen/MemoryOverlap.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
@@ -63,6 +64,13 @@ void* bytes(const at::Tensor& t, const char* where, const char* name, int64_t at
   TORCH_CHECK(t.device() == dev && t.is_cuda() && t.is_contiguous(), where, ": ", name, " is on ", t.device(), ", not contiguous on ", dev);
   TORCH_CHECK((int64_t)t.nbytes() >= at_least, where, ": ", name, " has ", t.nbytes(), " bytes, too small for ", at_least);
   return t.data_ptr();
+}
+
+// A result that other threads still read or write something else through: refused as far as that is seen (not between interleaved views).
+void apart(const at::Tensor& a, const at::Tensor& b, const char* where, const char* name, const char* other) {
+  const at::MemOverlapStatus s = at::get_overlap_status(a, b);
+  TORCH_CHECK(s != at::MemOverlapStatus::Full && s != at::MemOverlapStatus::Partial && (a.numel() == 0 || a.data_ptr() != b.data_ptr()), where, ": ", name, " and ", other,
+              " share memory");
 }
 
 // A checkpoint's buffer: the codes, then the scales.
@@ -152,6 +160,7 @@ PyObject* gemv(PyObject*, Args a, Py_ssize_t n) {
   TORCH_CHECK(W.R >= 0, where, ": ", W.R, " weight rows");
   at::Tensor Y = given(a[13]) ? tensor(a[13], where, "out") : matrix(M, W.R, X.options().dtype(type));
   const int64_t ldy = rows_of(Y, where, "out", type, M, W.R, dev);
+  if (given(a[13])) apart(Y, X, where, "out", "X");
   const size_t need = nvfp4_gemv_workspace_bytes(M, D, n_out);
   const at::Tensor ws = need ? at::empty({(int64_t)need}, X.options().dtype(at::kByte)) : at::Tensor();
   enqueue(where, [&] { return nvfp4_gemv(X.data_ptr(), ldx, M, D, &W, keep, outl, n_out, W_out, bias, Y.data_ptr(), code_of(type), ldy, status, need ? ws.data_ptr() : nullptr, need,
@@ -246,6 +255,7 @@ PyObject* swiglu_bwd(PyObject*, Args a, Py_ssize_t n) {
   }
   at::Tensor dG = given(a[7]) ? tensor(a[7], where, "dG") : matrix(T, D, dH.options()), dU = given(a[8]) ? tensor(a[8], where, "dU") : matrix(T, D, dH.options());
   const int64_t lddg = rows_of(dG, where, "dG", at::kBFloat16, T, D, dev), lddu = rows_of(dU, where, "dU", at::kBFloat16, T, D, dev);
+  if (given(a[7]) || given(a[8])) apart(dG, dU, where, "dG", "dU");
   enqueue(where, [&] { return nvfp4_swiglu_bwd(dH.data_ptr(), lddh, G, ldg, U, ldu, packed ? &cg : nullptr, packed ? &cu : nullptr, T, D, dG.data_ptr(), lddg, dU.data_ptr(), lddu, current_stream()); });
   return tuple_of(dG, dU);
   END_HANDLE_TH_ERRORS
