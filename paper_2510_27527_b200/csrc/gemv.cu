@@ -631,9 +631,10 @@ nvfp4_status nvfp4_gemv_ex(const void* X_bf16, int64_t ldx, int64_t M, int64_t D
   const int64_t row_ctas = (W->R + kRows - 1) / kRows, most = (int64_t)device_sm_count() * 2;
   const int S = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(kMaxCluster, a.n_pairs), most / row_ctas));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // Three and four tokens: as one and two (in two columns of instructions each) where every CTA has a single pair and a launch more is what counts:
-  // us from Python, 1024 x 2816 times three 6.8 against 8.7; on the device alone 8192 x 8192 17.5 against 14.5, 4096 x 4096 7.7 against 7.8.
-  const bool few = M <= 4 && row_ctas * a.n_pairs <= most;
+  // Three and four tokens: as one and two (in two columns of instructions each) where one wave of CTAs has two pairs each at most and a launch more is
+  // what counts: us from Python / on the device, times three, 1024 x 2816 5.4 / 5.0 against 6.8 / 5.1 with the launch, 1024 x 4096 5.6 / 5.1 against
+  // 6.5 / 5.2; with four pairs 1024 x 8192 7.7 / 7.6 against 7.1 / 6.9, with fifteen 128 x 30000 18.4 / 18.3 against 13.0 / 12.6.
+  const bool few = M <= 4 && row_ctas * a.n_pairs <= most && a.n_pairs <= 2 * S;
   const cudaError_t e = M <= 2    ? launch_gemv<1, true>(codes, outliers, a, row_ctas, S, st)
                         : few     ? launch_gemv<2, true>(codes, outliers, a, row_ctas, S, st)
                         : M <= 8  ? launch_gemv<1, false>(codes, outliers, a, row_ctas, S, st)
