@@ -56,9 +56,8 @@ struct GemvArgs {
   int64_t ldx, M;
   int D, K;  // columns of X, of the operand
   const int32_t *keep, *outl;
-  int n_out, Kh;
-  const uint16_t* W_out;
-  const uint8_t *codes, *sf;
+  int n_out;
+  const uint8_t* sf;
   const float* gscale;
   int64_t N;
   int gs_mode;
@@ -608,9 +607,6 @@ nvfp4_status nvfp4_gemv_ex(const void* X_bf16, int64_t ldx, int64_t M, int64_t D
   a.keep = n_out > 0 ? keep_cols : nullptr;
   a.outl = n_out > 0 ? outlier_cols : nullptr;
   a.n_out = (int)n_out;
-  a.Kh = (int)nvfp4_outlier_pad(n_out);
-  a.W_out = static_cast<const uint16_t*>(W_out);
-  a.codes = W->codes;
   a.sf = W->sf;
   a.gscale = W->gscale;
   a.N = W->R;
@@ -626,7 +622,7 @@ nvfp4_status nvfp4_gemv_ex(const void* X_bf16, int64_t ldx, int64_t M, int64_t D
   a.wait_limit = opts && opts->wait_limit_cycles > 0 ? opts->wait_limit_cycles : DEFAULT_WAIT_LIMIT_CYCLES;
   a.starve = opts && opts->starve_first_stage;
   CUtensorMap codes{}, outliers{};
-  if (!encode_codes_map(&codes, W->codes, W->R, nvfp4_padded_k(W->K)) || (n_out > 0 && !encode_outliers_map(&outliers, W_out, W->R, a.Kh))) return NVFP4_ERR_CUDA;
+  if (!encode_codes_map(&codes, W->codes, W->R, nvfp4_padded_k(W->K)) || (n_out > 0 && !encode_outliers_map(&outliers, W_out, W->R, nvfp4_outlier_pad(n_out)))) return NVFP4_ERR_CUDA;
   // CTAs along k: as many as leave every CTA a pair and give an SM two of them
   const int64_t row_ctas = (W->R + kRows - 1) / kRows, most = (int64_t)device_sm_count() * 2;
   const int S = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(kMaxCluster, a.n_pairs), most / row_ctas));

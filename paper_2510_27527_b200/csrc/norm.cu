@@ -396,34 +396,40 @@ __global__ void __launch_bounds__(1024) norm_bwd_finish_kernel(const float* __re
   store_grad(blockIdx.y ? dbeta : dgamma, f32, c, t);
 }
 
-// The shape of a row's group: as few threads as hold the row in MOST vectors each (three in forward, two in backward, whose registers hold
-// the columns' sums too), more vectors in the largest rows.
-template <int MOST, typename F>
-auto with_shape(int D, F&& f) {
-  using std::integral_constant;
-  const int n8 = (D + 7) / 8;
-  if (n8 <= 32) return f(integral_constant<int, 1>{}, integral_constant<int, 32>{});
-  if (n8 <= 64) return f(integral_constant<int, 2>{}, integral_constant<int, 32>{});
-  if (MOST >= 3 && n8 <= 96) return f(integral_constant<int, MOST>{}, integral_constant<int, 32>{});
-  if (n8 <= 128) return f(integral_constant<int, 2>{}, integral_constant<int, 64>{});
-  if (MOST >= 3 && n8 <= 192) return f(integral_constant<int, MOST>{}, integral_constant<int, 64>{});
-  if (n8 <= 256) return f(integral_constant<int, 2>{}, integral_constant<int, 128>{});
-  if (MOST >= 3 && n8 <= 384) return f(integral_constant<int, MOST>{}, integral_constant<int, 128>{});
-  if (n8 <= 512) return f(integral_constant<int, 2>{}, integral_constant<int, 256>{});
-  if (MOST >= 3 && n8 <= 768) return f(integral_constant<int, MOST>{}, integral_constant<int, 256>{});
-  if (n8 <= 1024) return f(integral_constant<int, 2>{}, integral_constant<int, 512>{});
-  if (n8 <= 1536) return f(integral_constant<int, 3>{}, integral_constant<int, 512>{});
-  return f(integral_constant<int, 4>{}, integral_constant<int, 512>{});
-}
+template <int N>
+using Int = std::integral_constant<int, N>;
 
-// Forward's: a warp holds up to 1024 elements, so that most rows need no barrier.
+// The shape of a row's group, as (vectors of eight a thread, threads): as few threads as hold the row in three vectors each, in up to four vectors
+// up to 1024 elements, which one warp holds, so that most rows need no barrier, and in the largest rows.
 template <typename F>
 auto with_fwd_shape(int D, F&& f) {
-  using std::integral_constant;
   const int n8 = (D + 7) / 8;
-  if (n8 > 64 && n8 <= 96) return f(integral_constant<int, 3>{}, integral_constant<int, 32>{});
-  if (n8 > 64 && n8 <= 128) return f(integral_constant<int, 4>{}, integral_constant<int, 32>{});
-  return with_shape<3>(D, f);
+  if (n8 <= 32) return f(Int<1>{}, Int<32>{});
+  if (n8 <= 64) return f(Int<2>{}, Int<32>{});
+  if (n8 <= 96) return f(Int<3>{}, Int<32>{});
+  if (n8 <= 128) return f(Int<4>{}, Int<32>{});
+  if (n8 <= 192) return f(Int<3>{}, Int<64>{});
+  if (n8 <= 256) return f(Int<2>{}, Int<128>{});
+  if (n8 <= 384) return f(Int<3>{}, Int<128>{});
+  if (n8 <= 512) return f(Int<2>{}, Int<256>{});
+  if (n8 <= 768) return f(Int<3>{}, Int<256>{});
+  if (n8 <= 1024) return f(Int<2>{}, Int<512>{});
+  if (n8 <= 1536) return f(Int<3>{}, Int<512>{});
+  return f(Int<4>{}, Int<512>{});
+}
+
+// Backward's: in two vectors, since its registers hold the columns' sums too, more in the largest rows.
+template <typename F>
+auto with_bwd_shape(int D, F&& f) {
+  const int n8 = (D + 7) / 8;
+  if (n8 <= 32) return f(Int<1>{}, Int<32>{});
+  if (n8 <= 64) return f(Int<2>{}, Int<32>{});
+  if (n8 <= 128) return f(Int<2>{}, Int<64>{});
+  if (n8 <= 256) return f(Int<2>{}, Int<128>{});
+  if (n8 <= 512) return f(Int<2>{}, Int<256>{});
+  if (n8 <= 1024) return f(Int<2>{}, Int<512>{});
+  if (n8 <= 1536) return f(Int<3>{}, Int<512>{});
+  return f(Int<4>{}, Int<512>{});
 }
 
 template <int SRC, bool CK>
@@ -440,7 +446,7 @@ cudaError_t launch_norm_fwd(const NormFwdArgs& a, cudaStream_t st) {
 }
 
 int bwd_ctas(int64_t T, int D) {
-  return with_shape<2>(D, [&](auto, auto tpr) {
+  return with_bwd_shape(D, [&](auto, auto tpr) {
     constexpr int GROUPS = kBwdThreads / decltype(tpr)::value;
     // (up to two rows a group, one CTA without the second launch: us from Python, 16 x 1024 7.4 against 10.8)
     return T <= 2 * GROUPS ? 1 : (int)std::min<int64_t>((T + GROUPS - 1) / GROUPS, kBwdCtas);
@@ -449,7 +455,7 @@ int bwd_ctas(int64_t T, int D) {
 
 template <int SRC>
 cudaError_t launch_norm_bwd(const NormBwdArgs& a, int ctas, cudaStream_t st) {
-  return with_shape<2>(a.D, [&](auto nv, auto tpr) {
+  return with_bwd_shape(a.D, [&](auto nv, auto tpr) {
     constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value, GROUPS = kBwdThreads / TPR;
     constexpr size_t smem = (2 * kSlots + (size_t)GROUPS * NV * 4 * TPR) * sizeof(f32x2);  // slots; gamma, or the sums of half the groups
     auto kernel = a.D % 8 ? norm_bwd_kernel<SRC, NV, TPR, false> : norm_bwd_kernel<SRC, NV, TPR, true>;
