@@ -32,7 +32,7 @@ def _bf16(x: torch.Tensor) -> torch.Tensor:
 
 def _save(ctx, checkpoint: bool) -> int:
     """What a call keeps. (Nothing where it goes through its function for a trace alone.)"""
-    return B.SAVE_NOTHING if not any(ctx.needs_input_grad) else B.SAVE_CKPT8 if checkpoint else B.SAVE_INPUT
+    return (B.SAVE_CKPT8 if checkpoint else B.SAVE_INPUT) if True in ctx.needs_input_grad else B.SAVE_NOTHING
 
 
 class _LayerNormFn(torch.autograd.Function):
@@ -87,23 +87,20 @@ class _FrozenFn(torch.autograd.Function):
         raise RuntimeError("NVFP4FrozenLinear has no gradient")
 
 
-@torch.compiler.disable
-def _frozen(*args):
-    return _FrozenFn.apply(*args) if _needs_function(*args[:8]) else _gemv(*args)
-
-
-@torch.compiler.disable  # (a compiler would not see what the library writes)
-def _layer_norm(x, gamma, beta, eps, checkpoint):
+def _layer_norm_call(x, gamma, beta, eps, checkpoint):
     if _needs_function(x, gamma, beta):
         return _LayerNormFn.apply(x, gamma, beta, eps, checkpoint)
     return B.nvfp4_layernorm_fwd(x, gamma, beta, eps, B.SAVE_NOTHING)[0]
 
 
-@torch.compiler.disable
-def _swiglu(g, u, checkpoint):
+def _swiglu_call(g, u, checkpoint):
     if _needs_function(g, u):
         return _SwigluFn.apply(g, u, checkpoint)
     return B.nvfp4_swiglu_fwd(g, u, B.SAVE_NOTHING)[0]
+
+
+# (a compiler would not see what the library writes)
+_layer_norm, _swiglu = torch.compiler.disable(_layer_norm_call), torch.compiler.disable(_swiglu_call)
 
 
 def swiglu(g: torch.Tensor, u: torch.Tensor, checkpoint: bool = True) -> torch.Tensor:
@@ -165,8 +162,10 @@ class NVFP4FrozenLinear(_Frozen):
         if _wants_grad(x):
             raise RuntimeError("NVFP4FrozenLinear has no gradient: use it under torch.no_grad()")
         rows = _rows(_bf16(x), self.in_features, "NVFP4FrozenLinear")
-        y = _frozen(rows, self.codes, self.scales, self.global_scales, self.outlier_cols, self.keep_cols, self.outlier_weight, self.bias,
-                    (self.out_features, self.in_features - self.n_out, self.gs_mode, self.dev_status))
+        h = self._buffers  # (a module's own look-up is slower: 2 us for the seven)
+        args = (rows, h["codes"], h["scales"], h["global_scales"], h["outlier_cols"], h["keep_cols"], h["outlier_weight"], h["bias"],
+                (self.out_features, self.in_features - self.n_out, self.gs_mode, self.dev_status))
+        y = _FrozenFn.apply(*args) if _needs_function(rows, args[3], args[6], args[7]) else _gemv(*args)
         return y if x.dim() == 2 else y.reshape(*x.shape[:-1], self.out_features)
 
 
@@ -207,6 +206,6 @@ class NVFP4FrozenMLP(_Frozen):
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         if _wants_grad(x):
             raise RuntimeError("NVFP4FrozenMLP has no gradient: use it under torch.no_grad()")
-        n = _layer_norm(_rows(x, self.features, "NVFP4FrozenMLP"), self.norm_weight, self.norm_bias, self.eps, False)
-        y = self.down(_swiglu(self.gate(n), self.up(n), False))
+        n = _layer_norm_call(_rows(x, self.features, "NVFP4FrozenMLP"), self.norm_weight, self.norm_bias, self.eps, False)
+        y = self.down(_swiglu_call(self.gate(n), self.up(n), False))
         return y if x.dim() == 2 else y.reshape(x.shape)

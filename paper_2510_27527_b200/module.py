@@ -103,7 +103,11 @@ def _plain(x: torch.Tensor, weight: torch.Tensor) -> bool:
 
 
 def _wants_grad(*tensors) -> bool:
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
 
 
 def _needs_function(*tensors) -> bool:
