@@ -142,3 +142,26 @@ def test_inputs_kept_elsewhere(width, checkpoint):
     with torch.autograd.graph.save_on_cpu():
         y, grads = step()
     assert all(torch.equal(p, q) for p, q in zip(grads(), want))
+
+
+@pytest.mark.parametrize("backend", ["eager", "inductor"])
+@pytest.mark.parametrize("checkpoint", [False, True])
+def test_compiled_autograd(checkpoint, backend):
+    from torch._dynamo import compiled_autograd
+
+    from paper_2510_27527_b200.block import NVFP4LayerNorm, swiglu
+
+    torch._dynamo.reset()
+    ln, dy, got = NVFP4LayerNorm(64, checkpoint=checkpoint), mk(6, 64), []
+    x = mk(6, 64).requires_grad_()
+    for compiled in (False, True, True):
+        x.grad = ln.weight.grad = ln.bias.grad = None
+        y = swiglu(ln(x), x, checkpoint)
+        if compiled:
+            with compiled_autograd._enable(torch.compile(backend=backend)):
+                y.backward(dy)
+        else:
+            y.backward(dy)
+        got.append((y.detach(), x.grad, ln.weight.grad, ln.bias.grad))
+    assert all(torch.equal(p, q) for g in got[1:] for p, q in zip(got[0], g))
+    torch._dynamo.reset()
