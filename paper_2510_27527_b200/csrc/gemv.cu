@@ -410,13 +410,20 @@ __global__ void __launch_bounds__(kThreads, MT > 2 ? 1 : 2) gemv_kernel(const __
             }
 #pragma unroll
             for (int n = 0; n < MT; ++n) {
-              const float x0 = shared_f32(xsc + 8 * n);
+              const f32x2 r = pair_of(shared_f32(xsc + 8 * n));
 #pragma unroll
               for (int k = 0; k < KB; ++k)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {  // column 2 t + (e & 1): lane (2 t + (e & 1)) & 3 of token 2 n + (t >> 1)
-                  const float2 scale = __half22float2(*reinterpret_cast<const __half2*>(&sc[2 * (k0 + k) + (e >> 1)][e & 1]));
-                  acc[k0 + k][n][e] = fmaf(fmaf(d[n][k][1][e], scale.y, d[n][k][0][e] * scale.x) * x0, x0 * gv[2 * (k0 + k) + (e >> 1)], acc[k0 + k][n][e]);
+                for (int e = 0; e < 4; e += 2) {  // columns 2 t and 2 t + 1: lanes (2 t) & 3 and the next of token 2 n + (t >> 1)
+                  const int j = 2 * (k0 + k) + (e >> 1);
+                  float2 scale[2];
+#pragma unroll
+                  for (int c = 0; c < 2; ++c) scale[c] = __half22float2(*reinterpret_cast<const __half2*>(&sc[j][c]));
+                  const f32x2 v = fma2(pair_of(d[n][k][1][e], d[n][k][1][e + 1]), pair_of(scale[0].y, scale[1].y),
+                                       mul2(pair_of(d[n][k][0][e], d[n][k][0][e + 1]), pair_of(scale[0].x, scale[1].x)));
+                  const float2 sum = values_of(fma2(mul2(v, r), mul2(r, pair_of(gv[j])), pair_of(acc[k0 + k][n][e], acc[k0 + k][n][e + 1])));
+                  acc[k0 + k][n][e] = sum.x;
+                  acc[k0 + k][n][e + 1] = sum.y;
                 }
             }
           }
@@ -439,14 +446,15 @@ __global__ void __launch_bounds__(kThreads, MT > 2 ? 1 : 2) gemv_kernel(const __
           }
 #pragma unroll
           for (int n = 0; n < MT; ++n) {
-            const float x0 = shared_f32(xsc + n * 32), x1 = shared_f32(xsc + n * 32 + 4);
+            const f32x2 r = pair_of(shared_f32(xsc + n * 32), shared_f32(xsc + n * 32 + 4));
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              acc[k][n][0] = fmaf(d[k][n][0] * x0, x0 * gv[2 * k], acc[k][n][0]);
-              acc[k][n][1] = fmaf(d[k][n][1] * x1, x1 * gv[2 * k], acc[k][n][1]);
-              acc[k][n][2] = fmaf(d[k][n][2] * x0, x0 * gv[2 * k + 1], acc[k][n][2]);
-              acc[k][n][3] = fmaf(d[k][n][3] * x1, x1 * gv[2 * k + 1], acc[k][n][3]);
-            }
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int e = 0; e < 4; e += 2) {
+                const float2 sum = values_of(fma2(mul2(pair_of(d[k][n][e], d[k][n][e + 1]), r), mul2(r, pair_of(gv[2 * k + (e >> 1)])), pair_of(acc[k][n][e], acc[k][n][e + 1])));
+                acc[k][n][e] = sum.x;
+                acc[k][n][e + 1] = sum.y;
+              }
           }
         } else if (!code) {  // 32 outlier channels
 #pragma unroll
