@@ -1,7 +1,8 @@
-"""What stands around the NVFP4 linears of a block, as torch modules: `NVFP4LayerNorm` (a drop-in nn.LayerNorm over the last dimension), `swiglu`,
-`NVFP4MLP` (norm, gate and up projections, SwiGLU, down projection) and, for answering token by token, `NVFP4FrozenLinear` / `NVFP4FrozenMLP`, whose
-weights are quantized once. For backward the norm and SwiGLU keep their inputs in 8 bits (1.03 bytes an element instead of 2), or with
-checkpoint=False the inputs themselves; the linears keep their FP4 operands. Argument marshalling only: every step runs in the library's kernels.
+"""What stands around the NVFP4 linears of a block, as torch modules: `NVFP4LayerNorm` (layer norm over the last dimension), `swiglu`, `NVFP4MLP`
+(layer norm, gate and up projections, SwiGLU, down projection) and, for answering token by token, `NVFP4FrozenLinear` / `NVFP4FrozenMLP`, whose
+weights are quantized once. For backward the norm and SwiGLU keep their inputs in 8 bits (1.03 bytes an element instead of 2): gradients are then
+those at the rounded inputs. With checkpoint=False they keep the inputs themselves. The linears keep their FP4 operands. Argument marshalling only:
+every step runs in the library's kernels.
 """
 from __future__ import annotations
 
@@ -104,7 +105,7 @@ _layer_norm, _swiglu = torch.compiler.disable(_layer_norm_call), torch.compiler.
 
 
 def swiglu(g: torch.Tensor, u: torch.Tensor, checkpoint: bool = True) -> torch.Tensor:
-    """silu(g) * u of two BF16 tensors of the same shape, with gradients. `checkpoint`: backward reads both in 8 bits."""
+    """silu(g) * u of two BF16 tensors of the same shape, with gradients. `checkpoint`: they are those at g and u rounded to 8 bits."""
     if g.shape != u.shape or g.dtype != torch.bfloat16 or u.dtype != torch.bfloat16:
         raise RuntimeError(f"swiglu: {g.dtype} {tuple(g.shape)} and {u.dtype} {tuple(u.shape)}, not two BF16 tensors of one shape")
     D = g.shape[-1] if g.dim() else 0
@@ -113,7 +114,8 @@ def swiglu(g: torch.Tensor, u: torch.Tensor, checkpoint: bool = True) -> torch.T
 
 
 class NVFP4LayerNorm(torch.nn.Module):
-    """Layer norm over the last dimension, BF16 or FP32 in, BF16 out; the parameters' sums and the statistics are FP32."""
+    """Layer norm over the last dimension with nn.LayerNorm's parameters, BF16 or FP32 in, BF16 out; the parameters' sums and the statistics are FP32.
+    `checkpoint`: gradients are those at the input rounded to 8 bits."""
 
     def __init__(self, features: int, eps: float = 1e-5, bias: bool = True, checkpoint: bool = True, dtype: torch.dtype = torch.bfloat16, device="cuda"):
         super().__init__()
@@ -142,7 +144,8 @@ class _Frozen(torch.nn.Module):
 
 class NVFP4FrozenLinear(_Frozen):
     """y = x W-hat^T (+ bias) with the weights as NVFP4Linear's forward quantizes them (OutControl's outlier channels in high precision) and x in
-    BF16: for answering, a few tokens at a time. No gradients. A wait that runs out is reported in the layer's cfg.dev_status, as in training."""
+    BF16: for answering, a few tokens at a time (every 32 are a pass over the weights; a prompt goes faster through the layer itself, with x in FP4).
+    No gradients. A wait that runs out is reported in the layer's cfg.dev_status, as in training."""
 
     def __init__(self, layer: NVFP4Linear):
         super().__init__()
@@ -170,8 +173,9 @@ class NVFP4FrozenLinear(_Frozen):
 
 
 class NVFP4MLP(torch.nn.Module):
-    """down(silu(gate(n)) * up(n)), n = norm(x): the MLP of a pre-norm block with NVFP4 linears (the caller adds the residual). `cfg` configures the
-    gate and up projections, `down_cfg` the down projection (default: cfg without its outlier channels, which are channels of x)."""
+    """down(silu(gate(n)) * up(n)), n = norm(x): the MLP of a block with layer norm in front and NVFP4 linears (the caller adds the residual). Blocks with
+    another norm take the parts: `swiglu` between three `NVFP4Linear`. `cfg` configures the gate and up projections, `down_cfg` the down projection
+    (default: cfg without its outlier channels, which are channels of x)."""
 
     def __init__(self, hidden: int, ffn: int, cfg: B.LayerConfig | None = None, down_cfg: B.LayerConfig | None = None, checkpoint: bool = True, eps: float = 1e-5,
                  norm_bias: bool = True, norm_dtype: torch.dtype = torch.bfloat16, device="cuda"):

@@ -4,9 +4,8 @@
 // The work is reading the weights, so all else is kept off their way. A warp takes 32 weight rows x 128 k at a time, 16 bytes (32 codes) of four
 // rows per lane, and multiplies them on the tensor cores (mma m16n8k16: 8 tokens cost what one costs; tcgen05 would want codes that somebody has
 // expanded into shared memory, or X in FP4): E2M1 pairs become FP16 pairs in one conversion each, times the block scale exactly (P * Sb has at
-// most 7 significant bits and lies within FP16's normal range). Those multiplications share a pipe with the matrix instructions: in a loop of
-// its own two words of codes take 34 cycles of a sub-partition with them, 23 without (conversions 16, matrix instructions 16). Up to two tokens,
-// where an instruction's other columns are free, sums of one block each are scaled instead (SEP below). Which k stand
+// most 7 significant bits and lies within FP16's normal range). Those multiplications are as many as the conversions and lengthen the chain to
+// the matrix instruction. Up to two tokens, where an instruction's other columns are free, sums of one block each are scaled instead (SEP below). Which k stand
 // in which slot of an instruction is free as long as both operands agree, so the codes are used as they lie in memory and X is staged in
 // shared memory in that order. FP16 also holds X: a token's 128 values are divided by the power of four r^2 that brings their largest magnitude
 // to [2^14, 2^16); a BF16 value has 8 significant bits, so the largest stays below FP16's end, the scaling is exact for all down to 2^-28 of
@@ -21,11 +20,13 @@
 // shared memory and added in a fixed order. Waits are for copies alone, and bounded.
 //
 // Measured (us, weights from HBM, replayed from a graph; the weights alone at the copy bandwidth in brackets): 1024 x 1024 times one token 3.0
-// (0.1), 4096 x 4096 5.9 (1.5), 8192 x 8192 11.2 (5.8); times 8 with 1x128 outer blocks 15.5, times 16 17.6, times 32 29; 14336 x 4096 times
-// 16 18.1 (5.2). What bounds it: for one token the chain of a warp's conversions and matrix instructions at 0.45 of the issue slots, and what a
-// short kernel begins and ends with (2 us until X is staged and the first weights are there, 1.5 for the cluster's sums); for more tokens the pipe
-// above. Measured and not better: rows through each warp's own ring of asynchronous copies (14.6 for 8192 x 8192 times one), three CTAs
-// to an SM (13.6), more CTAs than fit at once (16.6), X staged by every CTA for 16 tokens (24.8 against 17.6).
+// (0.1), 4096 x 4096 5.9 (1.5), 8192 x 8192 11.3 (5.8); times 8 with 1x128 outer blocks 15.5, times 16 17.6, times 32 30.3; 14336 x 4096 times
+// 16 17.8 (5.2). What bounds it: for one token the chain of a warp's conversions and matrix instructions at 0.44 of the issue slots, what a
+// short kernel begins and ends with (2 us until X is staged and the first weights are there, 1.5 for the cluster's sums), and 256 CTAs on 148
+// SMs; for more tokens the multiplications with the block scales, and above 16 a second wave of CTAs (below). Measured and not better: rows
+// through each warp's own ring of asynchronous copies (14.6 for 8192 x 8192 times one), three CTAs to an SM (13.6), more CTAs than fit at once
+// (16.6), X staged by every CTA for 16 tokens (24.8 against 17.6). Every 32 tokens are a pass over the weights: this is no form for a prompt
+// (8192 x 8192 times 64 58, times 2048 1700, where the library's quantizer and FP4 GEMM take 15 and 69).
 #include "../../include/nvfp4.h"
 
 #include "act8.cuh"
@@ -631,7 +632,8 @@ nvfp4_status nvfp4_gemv_ex(const void* X_bf16, int64_t ldx, int64_t M, int64_t D
   a.starve = opts && opts->starve_first_stage;
   CUtensorMap codes{}, outliers{};
   if (!encode_codes_map(&codes, W->codes, W->R, nvfp4_padded_k(W->K)) || (n_out > 0 && !encode_outliers_map(&outliers, W_out, W->R, nvfp4_outlier_pad(n_out)))) return NVFP4_ERR_CUDA;
-  // CTAs along k: as many as leave every CTA a pair and give an SM two of them
+  // CTAs along k: as many as leave every CTA a pair and are two to an SM together. (Of more than 16 tokens an SM holds one, so that they are up to
+  // two waves there: 256 for 8192 x 8192.)
   const int64_t row_ctas = (W->R + kRows - 1) / kRows, most = (int64_t)device_sm_count() * 2;
   const int S = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(kMaxCluster, a.n_pairs), most / row_ctas));
   cudaStream_t st = static_cast<cudaStream_t>(stream);

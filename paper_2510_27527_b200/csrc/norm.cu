@@ -7,12 +7,16 @@
 // the thread's columns). At the end the groups of a CTA add their column sums up in shared memory, the CTAs through a small FP32 matrix that a
 // second launch sums. Every sum has a fixed order.
 //
-// Measured (us, inputs from HBM, replayed from a graph; in brackets the share of the copy bandwidth), forward / backward: 16384 x 1024 BF16 14.2
-// (0.72) / 24.3 (0.64), with the checkpoint 17.7 (0.73) / 22.7 (0.57), 4096 x 4096 so 19.4 (0.67) / 24.2 (0.54), 2048 x 8192 so 20.7 (0.63) / 26.4
-// (0.49), FP32 4095 x 4096 19.4 (0.80) / 34.0 (0.76). Instructions bound it (0.55 - 0.57 of the issue slots, two thirds of them arithmetic in
-// pairs), with the chain through a row's sums; of backward about 4 us are the second launch. Registers decide the rest: forward gains from
-// warps (FP32 4095 x 4096 22.2 with 512 threads on an SM, 19.6 with 1024), backward loses more by spilling than they bring (16384 x 1024 23.6
-// with 128 registers, 52 with 85), and a row in one warp there holds too many sums (41.7).
+// Measured (us, inputs from HBM, replayed from a graph; in brackets the share of the copy bandwidth), forward / backward: 16384 x 1024 BF16 14.1
+// (0.73) / 23.5 (0.66), with the checkpoint 17.6 (0.74) / 22.2 (0.58), 4096 x 4096 so 19.1 (0.68) / 23.6 (0.55), 2048 x 8192 so 20.7 (0.62) / 26.3
+// (0.49), FP32 4095 x 4096 19.4 (0.80) / 34.3 (0.75). A row's chain through its sums bounds it, at 0.54 of the issue slots with a quarter of an
+// SM's warps; of backward about 4 us are the second launch. Registers decide the rest: forward gains from warps (FP32 4095 x 4096 22.2 with 512
+// threads on an SM, 19.6 with 1024), backward loses more by spilling than they bring (16384 x 1024 23.6 with 128 registers, 52 with 85), and a
+// row in one warp there holds too many sums (41.7). Where shapes spill it shows (2^24 elements as rows of so many columns, with the checkpoint):
+//   columns             1024   1500 (rows cut short)  2048   2816   4096   5120   8192   12288   16384
+//   BF16 forward        15.7   35.5                   18.8   20.6   18.8   22.5   20.0   22.4    38.2
+//   FP32 forward        24.2   36.1                   20.8   37.6   21.9   40.9   23.3   40.1    56.2
+//   BF16 backward       21.9   36.7                   22.5   25.9   23.5   28.7   26.2   35.8    54.2
 #include "../../include/nvfp4.h"
 
 #include "act8.cuh"
@@ -29,7 +33,8 @@ constexpr int kBwdThreads = 512, kBwdCtas = 148;
 
 template <int TPR>
 constexpr int kFwdThreadsOf = TPR < 128 ? 128 : TPR;  // of a CTA
-// Forward's threads per SM, by the registers that the shape needs (64 to 1024 threads, 96 to 640).
+// Forward's threads per SM, and so its registers a thread: 1024 threads have 64, 640 have 96. Shapes of three vectors (1025 to 1536, 2049 to 3072,
+// 4097 to 6144 columns) spill at 64, with BF16 rows 8 to 80 bytes, with FP32 rows 24 to 172, and the largest of four up to 276: see the times.
 template <int NV, int TPR>
 constexpr int kFwdThreadsPerSm = TPR == 32 && NV > 2 ? 640 : 1024;
 
