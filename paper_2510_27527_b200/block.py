@@ -147,6 +147,9 @@ class NVFP4FrozenLinear(_Frozen):
     BF16: for answering, a few tokens at a time (every 32 are a pass over the weights; a prompt goes faster through the layer itself, with x in FP4).
     No gradients. A wait that runs out is reported in the layer's cfg.dev_status, as in training."""
 
+    dev_status = None
+    _names = ("codes", "scales", "global_scales", "outlier_cols", "keep_cols", "outlier_weight", "bias")
+
     def __init__(self, layer: NVFP4Linear):
         super().__init__()
         self.in_features, self.out_features = layer.in_features, layer.out_features
@@ -166,6 +169,8 @@ class NVFP4FrozenLinear(_Frozen):
             raise RuntimeError("NVFP4FrozenLinear has no gradient: use it under torch.no_grad()")
         rows = _rows(_bf16(x), self.in_features, "NVFP4FrozenLinear")
         h = self._buffers  # (a module's own look-up is slower: 2 us for the seven)
+        if len(h) != len(self._names):  # (one is parametrized)
+            h = {n: getattr(self, n) for n in self._names}
         args = (rows, h["codes"], h["scales"], h["global_scales"], h["outlier_cols"], h["keep_cols"], h["outlier_weight"], h["bias"],
                 (self.out_features, self.in_features - self.n_out, self.gs_mode, self.dev_status))
         y = _FrozenFn.apply(*args) if _needs_function(rows, args[3], args[6], args[7]) else _gemv(*args)

@@ -165,3 +165,31 @@ def test_compiled_autograd(checkpoint, backend):
         got.append((y.detach(), x.grad, ln.weight.grad, ln.bias.grad))
     assert all(torch.equal(p, q) for g in got[1:] for p, q in zip(got[0], g))
     torch._dynamo.reset()
+
+
+def test_frozen_layers_with_a_parametrized_bias():
+    import torch.nn.utils.parametrize as parametrize
+
+    class Twice(torch.nn.Module):
+        def forward(self, v):
+            return 2 * v
+
+    f, g, x = frozen("linear"), frozen("linear"), mk(3, 64)
+    with torch.no_grad():
+        g.load_state_dict(f.state_dict())
+        f.bias.copy_(mk(40))
+        g.bias.copy_(2 * f.bias)
+        parametrize.register_parametrization(f, "bias", Twice())
+        assert torch.equal(f(x), g(x))
+
+
+@pytest.mark.parametrize("backend", ["eager", "inductor"])
+@pytest.mark.parametrize("kind", ["linear", "outliers", "mlp"])
+def test_compiled_frozen_modules(kind, backend):
+    torch._dynamo.reset()
+    f = frozen(kind)
+    with torch.no_grad():
+        g = torch.compile(f, backend=backend)
+        for x in (mk(3, 64), mk(3, 64), mk(7, 64)):
+            assert torch.equal(g(x), f(x))
+    torch._dynamo.reset()
